@@ -550,6 +550,125 @@ int32_t sdv2_attention_bf16(const void* q_dev, const void* const* k_dev, const v
                             void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * Ragged batches over a paged cache: streams and requests of different lengths in one list of rows, their keys and values in
+ * pages of one pool, norms per head, fewer key heads than query heads, an adapter per request.  An attention layer of such a
+ * batch is sdv2_gemm_bf16 (QKV), sdv2_lora_bf16, sdv2_paged_append, sdv2_paged_attention, sdv2_gemm_bf16, sdv2_lora_bf16.
+ *
+ * sdv2_ragged_batch: rows q_start[s] .. q_start[s + 1] - 1 (q_start[0] = 0, ascending) are the new tokens of sequence s, which has
+ *   kv_len[s] tokens with them; its i-th new token is its token kv_len[s] - (number of new ones) + i.  Token j lies in page
+ *   page_table[s][j / page_tokens], slot j % page_tokens.  A sequence may have no new token or no token at all.  The three arrays
+ *   are device memory, read when the kernels run: a recorded graph follows what they hold at each replay.  Rows from
+ *   q_start[n_seqs] up to n_tokens - 1 are padding: no output of theirs is written.  A table entry outside [0, n_pages) names no
+ *   page (given back, or not there yet): what would be appended to it is dropped, and its keys are in nobody's sight.
+ *   A kv_len above table_stride * page_tokens counts as that.  max_q_len and max_kv_len choose the form of a launch (and the
+ *   workspace); longer sequences are served all the same, less evenly spread.
+ * Pages: K and V each [n_pages][kv_heads][page_tokens][128], bf16, or e4m3 holding key / k_scale and value / v_scale.  A row of 128
+ *   numbers is read as it lies, so that one appended token is 256 (128) bytes in a row per head.
+ * Rows (q, k, v, o, x, y, out) are heads (columns) in a row of their own, `stride` elements from row to row.  Addresses are multiples
+ *   of 16 bytes and strides multiples of 8 elements, so views into the rows of a projection's output serve as they are.
+ * All of them: n_tokens = 0 is a batch without work (SDV2_OK, nothing launched).
+ * Errors: null pointers, wrong sizes, misaligned addresses, strides shorter than a row: SDV2_INVALID_ARG; SDV2_WORKSPACE_TOO_SMALL.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct sdv2_ragged_batch {
+    uint32_t struct_size;
+    int32_t n_seqs;               /* > 0 */
+    int32_t n_tokens;             /* rows of the list, padding included */
+    int32_t max_q_len;            /* most new tokens of a sequence, >= 0 */
+    int32_t max_kv_len;           /* most tokens of a sequence, >= 0 */
+    int32_t table_stride;         /* entries of a row of page_table, > 0 */
+    const int32_t* q_start;       /* dev [n_seqs + 1] */
+    const int32_t* kv_len;        /* dev [n_seqs], the new tokens included */
+    const int32_t* page_table;    /* dev [n_seqs][table_stride] */
+} sdv2_ragged_batch;
+
+#define SDV2_PAGES_BF16 0
+#define SDV2_PAGES_E4M3 1
+typedef struct sdv2_paged_cfg {
+    uint32_t struct_size;
+    int32_t kv_heads;             /* > 0 */
+    int32_t page_tokens;          /* 16, 32, 64, 128 or 256 */
+    int32_t n_pages;              /* > 0 */
+    int32_t format;               /* SDV2_PAGES_BF16 or SDV2_PAGES_E4M3 */
+    float k_scale, v_scale;       /* > 0; 1 for bf16 */
+} sdv2_paged_cfg;
+
+/* Bytes of EACH of the two pools (0 on a bad cfg). */
+size_t sdv2_paged_pool_bytes(const sdv2_paged_cfg* cfg);
+
+/* ------------------------------------------------------------------------------------------------
+ * sdv2_qk_norm_rope: for each row and head of q and of k (either may be NULL with 0 heads)
+ *     y = x / sqrt(mean(x^2) + eps) g      over the 128 numbers of the head (g NULL: y = x),
+ *   then the pairs turned by position * base^(-j / n): axes 0: none;  1: position pos[row], 64 pairs, j = 0 .. 63, n = 64;  3:
+ *   positions pos[row][0..2] (frame, row, column), 22, 21 and 21 pairs, j counted within the axis, n its pairs (the rotation of
+ *   sdv2_dit_block_forward).  pairs SDV2_PAIRS_ADJACENT: pair i is numbers 2 i and 2 i + 1; SDV2_PAIRS_HALVES: i and i + 64.
+ *   pos: dev int32 [n_tokens][axes], any value; angles are formed in 64 bits.  q_out / k_out may be q / k (in place); otherwise they
+ *   overlap nothing that is read.  Every one of the n_tokens rows is written.
+ * sdv2_paged_append: the same for k on its way to the pages of the batch's new tokens, v as it is, and (q not NULL) for q to q_out, in
+ *   one launch.  e4m3: key / k_scale and value / v_scale rounded once, beyond 448 to 448, NaN stays.  rope NULL: neither norm nor
+ *   rotation (keys are final; pos and gains NULL).  Two tokens of a call never share a slot (no page twice in the batch's tables).
+ * ------------------------------------------------------------------------------------------------ */
+#define SDV2_PAIRS_ADJACENT 0
+#define SDV2_PAIRS_HALVES 1
+typedef struct sdv2_rope_cfg {
+    uint32_t struct_size;
+    int32_t axes;                 /* 0, 1 or 3 */
+    int32_t pairs;                /* SDV2_PAIRS_ADJACENT or SDV2_PAIRS_HALVES */
+    float base;                   /* > 1 (10000) */
+    float eps;                    /* of the norm, > 0 (1e-6) */
+} sdv2_rope_cfg;
+int32_t sdv2_qk_norm_rope(const sdv2_rope_cfg* rope, int32_t n_tokens, const int32_t* pos_dev,
+                          const void* q_dev, int64_t q_stride, int32_t q_heads, const float* g_q_dev, void* q_out_dev, int64_t q_out_stride,
+                          const void* k_dev, int64_t k_stride, int32_t k_heads, const float* g_k_dev, void* k_out_dev, int64_t k_out_stride,
+                          void* hip_stream);
+int32_t sdv2_paged_append(const sdv2_paged_cfg* cfg, void* k_pages_dev, void* v_pages_dev, const sdv2_ragged_batch* batch,
+                          const sdv2_rope_cfg* rope, const int32_t* pos_dev,
+                          const void* k_dev, int64_t k_stride, const float* g_k_dev, const void* v_dev, int64_t v_stride,
+                          const void* q_dev, int64_t q_stride, int32_t q_heads, const float* g_q_dev, void* q_out_dev, int64_t q_out_stride,
+                          void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * sdv2_paged_attention: o = softmax(scale q K^T) V of the batch's rows over the keys each may see, q_heads a multiple of kv_heads
+ *   (query head h reads key head h / (q_heads / kv_heads)).  With L = kv_len of the sequence and p the row's token number, key j is seen if
+ *       j < e   and   (window = 0 or j >= e - window or j < sink),
+ *       e = L for block 0 (a chunk sees every token, its own included);  e = min(L, (p / block + 1) block) otherwise: block 1 is the
+ *       causal mask, block = tokens of a frame the frame-causal one.
+ *   A row that sees nothing is the zero row.  What keys and values hold where a row does not see them (infinities, NaN, storage never
+ *   written) does not reach it.
+ *   scale <= 0: 1 / sqrt(128).  o overlaps none of what is read.
+ * sdv2_paged_attention_workspace_bytes: for few rows and many keys, which are then shared out over the chip (0 where they are not).
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct sdv2_attn_mask {
+    uint32_t struct_size;
+    int32_t block;                /* >= 0 */
+    int32_t window;               /* >= 0; 0: none */
+    int32_t sink;                 /* >= 0; read with a window only */
+    float scale;
+} sdv2_attn_mask;
+size_t sdv2_paged_attention_workspace_bytes(const sdv2_paged_cfg* cfg, const sdv2_ragged_batch* batch, const sdv2_attn_mask* mask, int32_t q_heads);
+int32_t sdv2_paged_attention(const sdv2_paged_cfg* cfg, const void* k_pages_dev, const void* v_pages_dev, const sdv2_ragged_batch* batch,
+                             const sdv2_attn_mask* mask, const void* q_dev, int64_t q_stride, int32_t q_heads, void* o_dev, int64_t o_stride,
+                             void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
+ * sdv2_lora_bf16: the low-rank adapters of many requests beside a shared projection,
+ *     out[t] = y[t] + scale[i] (x[t] A_i^T) B_i^T,   i = adapter[s] of the row's sequence s;
+ *   an id outside [0, n_adapters) is no adapter: out[t] = y[t].  x: bf16 rows of K; A: bf16 [n_adapters][rank][K]; B: bf16
+ *   [n_adapters][N][rank]; scale: dev fp32 [n_adapters] or NULL (1); adapter: dev int32 [n_seqs]; q_start as in a ragged batch.
+ *   y, out: rows of N, bf16 (out_fp32 = 0) or fp32 (1); out may be y.  Sums are held in 32 bits; x A^T goes to the second product as two
+ *   bf16 numbers (16 bits of it).  K and N multiples of 64, rank a multiple of 8 up to 128.
+ * ------------------------------------------------------------------------------------------------ */
+typedef struct sdv2_lora_cfg {
+    uint32_t struct_size;
+    int32_t K, N, rank, n_adapters;
+    int32_t out_fp32;
+    int32_t n_seqs, n_tokens, max_q_len;      /* as in a ragged batch */
+} sdv2_lora_cfg;
+size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg);
+int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* b_dev, const float* scale_dev, const int32_t* adapter_dev,
+                       const int32_t* q_start_dev, const void* x_dev, int64_t x_stride, const void* y_dev, int64_t y_stride,
+                       void* out_dev, int64_t out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Per-launch timing for the benchmark (not part of the streaming path).  Between sdv2_prof_begin and
  * sdv2_prof_end every kernel launch site of sdv2_dit_block_forward / sdv2_denoise_step is bracketed by
  * a pair of HIP events on the caller's stream, up to max_samples launches.  sdv2_prof_end waits for

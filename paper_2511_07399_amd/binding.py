@@ -72,6 +72,30 @@ class MotionCfg(C.Structure):
                 ("s_min", C.c_float), ("s_max", C.c_float), ("s_init", C.c_float)]
 
 
+class PagedCfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("kv_heads", C.c_int32), ("page_tokens", C.c_int32), ("n_pages", C.c_int32),
+                ("format", C.c_int32), ("k_scale", C.c_float), ("v_scale", C.c_float)]
+
+
+class RaggedBatch(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_q_len", C.c_int32),
+                ("max_kv_len", C.c_int32), ("table_stride", C.c_int32), ("q_start", C.c_void_p), ("kv_len", C.c_void_p),
+                ("page_table", C.c_void_p)]
+
+
+class RopeCfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("axes", C.c_int32), ("pairs", C.c_int32), ("base", C.c_float), ("eps", C.c_float)]
+
+
+class AttnMask(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("block", C.c_int32), ("window", C.c_int32), ("sink", C.c_int32), ("scale", C.c_float)]
+
+
+class LoraCfg(C.Structure):
+    _fields_ = [("struct_size", C.c_uint32), ("K", C.c_int32), ("N", C.c_int32), ("rank", C.c_int32), ("n_adapters", C.c_int32),
+                ("out_fp32", C.c_int32), ("n_seqs", C.c_int32), ("n_tokens", C.c_int32), ("max_q_len", C.c_int32)]
+
+
 EXPORTS = (
     "sdv2_last_error", "sdv2_version", "sdv2_kv_cache_bytes", "sdv2_kv_cache_init", "sdv2_kv_cache_destroy",
     "sdv2_kv_cache_reset", "sdv2_kv_cache_append_evict", "sdv2_kv_cache_state", "sdv2_kv_cache_slot_map",
@@ -87,7 +111,8 @@ EXPORTS = (
     "sdv2_denoise_graph_launch", "sdv2_denoise_graph_destroy", "sdv2_timestep_vector", "sdv2_latent_io_workspace_bytes",
     "sdv2_patch_embed", "sdv2_output_head", "sdv2_noise_latents", "sdv2_sampler_update",
     "sdv2_denoise_latents_workspace_bytes", "sdv2_denoise_latents_step", "sdv2_stream_batch_latents_workspace_bytes",
-    "sdv2_stream_batch_latents_step",
+    "sdv2_stream_batch_latents_step", "sdv2_paged_pool_bytes", "sdv2_qk_norm_rope", "sdv2_paged_append",
+    "sdv2_paged_attention_workspace_bytes", "sdv2_paged_attention", "sdv2_lora_workspace_bytes", "sdv2_lora_bf16",
 )
 
 LAUNCH_TAGS = ("adaLN-1", "QKV gemm", "rope+append", "self-attn", "out-proj gemm", "LN-3", "cross-q gemm",
@@ -197,6 +222,18 @@ def load_library():
     lib.sdv2_stream_batch_latents_step.argtypes = [vp, C.POINTER(ModelCfg), C.POINTER(ModelWeights), C.POINTER(IoWeights), vp,
                                                    f32p, i32, fp, f32p, C.POINTER(vp), C.POINTER(vp), f32p,
                                                    C.POINTER(i32), C.POINTER(i32), vp, sz, vp]
+    i64 = C.c_int64
+    lib.sdv2_paged_pool_bytes.restype = sz
+    lib.sdv2_paged_pool_bytes.argtypes = [vp]
+    rows = [vp, i64, i32, f32p, vp, i64]                    # rows, stride, heads, gain, output, its stride
+    lib.sdv2_qk_norm_rope.argtypes = [vp, i32, vp] + rows + rows + [vp]
+    lib.sdv2_paged_append.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, f32p, vp, i64] + rows + [vp]
+    lib.sdv2_paged_attention_workspace_bytes.restype = sz
+    lib.sdv2_paged_attention_workspace_bytes.argtypes = [vp, vp, vp, i32]
+    lib.sdv2_paged_attention.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, vp, i64, vp, sz, vp]
+    lib.sdv2_lora_workspace_bytes.restype = sz
+    lib.sdv2_lora_workspace_bytes.argtypes = [vp]
+    lib.sdv2_lora_bf16.argtypes = [vp, vp, vp, f32p, vp, vp, vp, i64, vp, i64, vp, i64, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -730,3 +767,153 @@ def stream_batch_latents_step(h, cfg, mw, io, cache, z_in, frame_pos0, sigmas, e
                                                _timesteps(sigmas), _ptr(eps_by_depth), kt, vtt, _ptr(z_out),
                                                C.byref(emitted), C.byref(rows), _ptr(workspace), _nbytes(workspace), _stream()))
     return bool(emitted.value), rows.value
+
+
+# ------------------------------------------------------------------------------------------ ragged batches over a paged cache
+# Rows are 2-D tensors whose rows are contiguous, at any stride (slices of a projection's output serve as they are).  Whatever
+# lies on the device has to be on the current one: launches go to its current stream.
+_PAGE_DTYPE = {0: torch.bfloat16, 1: torch.float8_e4m3fn}
+
+
+def _here(t, dtype):
+    assert t.is_cuda and t.dtype == dtype and t.get_device() == _current_device(), "expected a %s tensor on the current device" % dtype
+    return t.data_ptr()
+
+
+def _dense(t, dtype):
+    assert t.is_contiguous(), "expected a contiguous tensor"
+    return _here(t, dtype)
+
+
+def _gain(t):
+    if t is None:
+        return None
+    assert t.numel() == HEAD_DIM, "a gain has 128 numbers"
+    return _dense(t, torch.float32)
+
+
+def _row_tensor(t, width=None, rows=None, dtype=torch.bfloat16):
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), "expected rows of contiguous elements"
+    assert (width is None or t.shape[1] == width) and (rows is None or t.shape[0] == rows), "rows of another shape than expected"
+    # the stride of a tensor of at most one row says nothing, and may be anything
+    return _here(t, dtype), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 8)
+
+
+def _heads(t, rows):
+    p, stride = _row_tensor(t, None, rows)
+    assert t.shape[1] % HEAD_DIM == 0, "rows are heads of 128"
+    return p, stride, t.shape[1] // HEAD_DIM
+
+
+def rope_cfg(axes, halves=False, base=10000.0, eps=1e-6):
+    """axes: 0 (no rotation), 1 (64 pairs) or 3 (frame, row, column: 22, 21, 21 pairs); halves: pairs (j, j + 64) instead of (2j, 2j + 1)."""
+    return RopeCfg(C.sizeof(RopeCfg), axes, int(halves), base, eps)
+
+
+def paged_cfg(kv_heads, page_tokens, n_pages, e4m3=False, k_scale=1.0, v_scale=1.0):
+    return PagedCfg(C.sizeof(PagedCfg), kv_heads, page_tokens, n_pages, int(e4m3), k_scale, v_scale)
+
+
+def paged_pool_bytes(cfg):
+    """Bytes of each of the two pools, tensors [n_pages, kv_heads, page_tokens, 128] of bfloat16 or float8_e4m3fn."""
+    load_library()
+    n = _lib.sdv2_paged_pool_bytes(C.byref(cfg))
+    if n == 0:
+        _check(INVALID_ARG)
+    return n
+
+
+def ragged_batch(q_start, kv_len, page_table, n_tokens, max_q_len, max_kv_len):
+    """q_start: device int32 [n_seqs + 1]; kv_len: device int32 [n_seqs], after the append; page_table: device int32
+    [n_seqs, entries].  The struct keeps the three tensors alive."""
+    n = kv_len.numel()
+    assert q_start.numel() == n + 1 and page_table.dim() == 2 and page_table.shape[0] == n, "arrays of different batches"
+    b = RaggedBatch(C.sizeof(RaggedBatch), n, n_tokens, max_q_len, max_kv_len, page_table.shape[1], _dense(q_start, torch.int32),
+                    _dense(kv_len, torch.int32), _dense(page_table, torch.int32))
+    b.tensors = (q_start, kv_len, page_table)
+    return b
+
+
+def attn_mask(block=0, window=0, sink=0, scale=0.0):
+    """block 0: every key; B: the row's block of B tokens and what is before it (1: causal).  scale 0: 1 / sqrt(128)."""
+    return AttnMask(C.sizeof(AttnMask), block, window, sink, scale)
+
+
+def _positions(rope, pos, rows):
+    if rope is None or rope.axes == 0:
+        return None
+    assert pos.numel() == rows * rope.axes, "positions are [rows, axes]"
+    return _dense(pos, torch.int32)
+
+
+def qk_norm_rope(rope, positions, q, q_out, g_q=None, k=None, k_out=None, g_k=None):
+    """q, k (either may be None): bf16 rows of heads; the outputs may be the inputs.  positions: device int32 [rows, axes]."""
+    load_library()
+    T = (k if q is None else q).shape[0]
+    qp, qs, qh = (None, 0, 0) if q is None else _heads(q, T)
+    kp, ks, kh = (None, 0, 0) if k is None else _heads(k, T)
+    qo, qos = (None, 0) if q is None else _row_tensor(q_out, q.shape[1], T)
+    ko, kos = (None, 0) if k is None else _row_tensor(k_out, k.shape[1], T)
+    _check(_lib.sdv2_qk_norm_rope(C.addressof(rope), T, _positions(rope, positions, T), qp, qs, qh, _gain(g_q), qo, qos,
+                                  kp, ks, kh, _gain(g_k), ko, kos, _stream()))
+
+
+def _pages(cfg, k_pages, v_pages):
+    shape = (cfg.n_pages, cfg.kv_heads, cfg.page_tokens, HEAD_DIM)
+    dtype = _PAGE_DTYPE[cfg.format]
+    assert tuple(k_pages.shape) == shape and tuple(v_pages.shape) == shape, "pools are [n_pages, kv_heads, page_tokens, 128]"
+    return _dense(k_pages, dtype), _dense(v_pages, dtype)
+
+
+def paged_append(cfg, k_pages, v_pages, batch, k, v, rope=None, positions=None, g_k=None, q=None, q_out=None, g_q=None):
+    """k, v: bf16 rows of the batch's new tokens.  With rope, k (and q, to q_out) get norm (with a gain) and rotation on the way."""
+    load_library()
+    T = batch.n_tokens
+    kp, vp = _pages(cfg, k_pages, v_pages)
+    kr, ks = _row_tensor(k, cfg.kv_heads * HEAD_DIM, T)
+    vr, vs = _row_tensor(v, cfg.kv_heads * HEAD_DIM, T)
+    qp, qs, qh = (None, 0, 0) if q is None else _heads(q, T)
+    qo, qos = (None, 0) if q is None else _row_tensor(q_out, q.shape[1], T)
+    _check(_lib.sdv2_paged_append(C.addressof(cfg), kp, vp, C.addressof(batch), None if rope is None else C.addressof(rope),
+                                  _positions(rope, positions, T), kr, ks, _gain(g_k), vr, vs, qp, qs, qh, _gain(g_q), qo, qos, _stream()))
+
+
+def paged_attention_workspace_bytes(cfg, batch, mask, q_heads):
+    load_library()
+    return _lib.sdv2_paged_attention_workspace_bytes(C.addressof(cfg), C.addressof(batch), C.addressof(mask), q_heads)
+
+
+def paged_attention(cfg, k_pages, v_pages, batch, mask, q, o, workspace=None):
+    """q, o: bf16 rows [n_tokens, q_heads * 128]."""
+    load_library()
+    T = batch.n_tokens
+    kp, vp = _pages(cfg, k_pages, v_pages)
+    qp, qs, qh = _heads(q, T)
+    op, os_ = _row_tensor(o, q.shape[1], T)
+    _check(_lib.sdv2_paged_attention(C.addressof(cfg), kp, vp, C.addressof(batch), C.addressof(mask), qp, qs, qh, op, os_, _ptr(workspace),
+                                     0 if workspace is None else workspace.nbytes, _stream()))
+
+
+def lora_cfg(K, N, rank, n_adapters, n_seqs, n_tokens, max_q_len, fp32=False):
+    return LoraCfg(C.sizeof(LoraCfg), K, N, rank, n_adapters, int(fp32), n_seqs, n_tokens, max_q_len)
+
+
+def lora_workspace_bytes(n_seqs, n_tokens, max_q_len, K, rank):
+    load_library()
+    return _lib.sdv2_lora_workspace_bytes(C.byref(lora_cfg(K, 64, rank, 1, n_seqs, n_tokens, max_q_len)))
+
+
+def lora_bf16(x, a, b, scale, adapter, q_start, max_q_len, y, out, workspace):
+    """out = y + scale (x A^T) B^T: a bf16 [n_adapters, rank, K], b bf16 [n_adapters, N, rank], scale fp32 [n_adapters] or None,
+    adapter int32 [n_seqs] (outside [0, n_adapters): none), q_start int32 [n_seqs + 1]; y and out of one type, bf16 or fp32."""
+    load_library()
+    n, rank, K = a.shape
+    N, T, fp32 = b.shape[1], x.shape[0], y.dtype == torch.float32
+    assert tuple(b.shape) == (n, N, rank) and q_start.numel() == adapter.numel() + 1 and (scale is None or scale.numel() == n), "shapes disagree"
+    xp, xs = _row_tensor(x, K, T)
+    yp, ys = _row_tensor(y, N, T, torch.float32 if fp32 else torch.bfloat16)
+    op, os_ = _row_tensor(out, N, T, y.dtype)
+    cfg = lora_cfg(K, N, rank, n, adapter.numel(), T, max_q_len, fp32)
+    _check(_lib.sdv2_lora_bf16(C.addressof(cfg), _dense(a, torch.bfloat16), _dense(b, torch.bfloat16),
+                               None if scale is None else _dense(scale, torch.float32), _dense(adapter, torch.int32), _dense(q_start, torch.int32),
+                               xp, xs, yp, ys, op, os_, _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))

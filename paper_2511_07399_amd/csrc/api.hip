@@ -1,6 +1,7 @@
 // Host side of libsdv2: argument validation, ring bookkeeping, workspace carving and the launch
 // sequence of the block.  See include/sdv2.h for the contract of every exported call.
 #include "common.h"
+#include "ragged.h"
 
 #include <math.h>
 #include <stdarg.h>
@@ -2034,6 +2035,309 @@ int32_t sdv2_prof_sample_kernel(int32_t sample, char* out, size_t capacity) {
     if (g_prof.on) return fail(SDV2_BAD_STATE, "profiling is still on");
     if (sample < 0 || (size_t)sample >= g_prof.kernel.size()) return fail(SDV2_INVALID_ARG, "no sample %d", sample);
     snprintf(out, capacity, "%s", g_prof.kernel[sample].c_str());
+    return SDV2_OK;
+}
+
+}  // extern "C"
+
+// ------------------------------------------------------------------------------------------ ragged batches over a paged cache
+namespace {
+
+constexpr int64_t kMostRowHeads = (int64_t)1 << 26;      // rows times heads of a call: a grid has fewer than 2^32 threads
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Rows of `width` elements at p, `stride` elements apart, of `size` bytes each.
+const char* rows_wrong(const void* p, int64_t stride, int64_t width, int size) {
+    if (!p) return "null pointer";
+    if (!aligned16(p)) return "address is not a multiple of 16 bytes";
+    if (stride < width) return "stride is shorter than a row";
+    if (stride * size % 16) return "stride is not a multiple of 16 bytes";
+    if (stride > ((int64_t)1 << 40)) return "stride is too large";
+    return nullptr;
+}
+
+const char* paged_cfg_wrong(const sdv2_paged_cfg* c) {
+    if (!c) return "cfg is null";
+    if (c->struct_size != sizeof(sdv2_paged_cfg)) return "cfg.struct_size mismatch";
+    if (c->kv_heads <= 0 || c->kv_heads > 65535) return "kv_heads out of range";
+    if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens must be 16, 32, 64, 128 or 256";
+    if (c->n_pages <= 0) return "n_pages must be positive";
+    if (c->format != SDV2_PAGES_BF16 && c->format != SDV2_PAGES_E4M3) return "unknown page format";
+    if (!(c->k_scale > 0.0f) || !(c->v_scale > 0.0f) || isinf(c->k_scale) || isinf(c->v_scale)) return "scales must be positive";
+    if (c->format == SDV2_PAGES_BF16 && (c->k_scale != 1.0f || c->v_scale != 1.0f)) return "bf16 pages have no scale";
+    return nullptr;
+}
+
+const char* batch_wrong(const sdv2_ragged_batch* b, const sdv2_paged_cfg* c) {
+    if (!b) return "batch is null";
+    if (b->struct_size != sizeof(sdv2_ragged_batch)) return "batch.struct_size mismatch";
+    if (b->n_seqs <= 0 || b->n_seqs > (1 << 24)) return "n_seqs out of range";
+    if (b->n_tokens < 0 || b->max_q_len < 0 || b->max_kv_len < 0) return "negative length";
+    if (b->table_stride <= 0 || (int64_t)b->table_stride * c->page_tokens > ((int64_t)1 << 30)) return "table_stride out of range";
+    return nullptr;
+}
+
+const char* batch_arrays_wrong(const sdv2_ragged_batch* b) { return b->q_start && b->kv_len && b->page_table ? nullptr : "null array in batch"; }
+
+RaggedArgs ragged_args(const sdv2_ragged_batch* b, const sdv2_paged_cfg* c) {
+    RaggedArgs r{};
+    r.q_start = b->q_start;
+    r.kv_len = b->kv_len;
+    r.table = b->page_table;
+    r.n_seqs = b->n_seqs;
+    r.n_tokens = b->n_tokens;
+    r.table_stride = b->table_stride;
+    while ((1 << r.page_shift) < c->page_tokens) ++r.page_shift;
+    r.n_pages = c->n_pages;
+    r.kv_heads = c->kv_heads;
+    return r;
+}
+
+const char* rope_wrong(const sdv2_rope_cfg* r) {
+    if (r->struct_size != sizeof(sdv2_rope_cfg)) return "rope.struct_size mismatch";
+    if (r->axes != 0 && r->axes != 1 && r->axes != 3) return "axes must be 0, 1 or 3";
+    if (r->pairs != SDV2_PAIRS_ADJACENT && r->pairs != SDV2_PAIRS_HALVES) return "unknown order of pairs";
+    if (!(r->base > 1.0f) || isinf(r->base) || !(r->eps > 0.0f)) return "base / eps out of range";
+    return nullptr;
+}
+
+void set_rotation(TurnArgs* a, const sdv2_rope_cfg* r, const int32_t* pos) {
+    a->axes = r->axes;
+    a->halves = r->pairs == SDV2_PAIRS_HALVES;
+    a->eps = r->eps;
+    a->pos = pos;
+    const int counts[3] = {r->axes == 1 ? 64 : 22, 21, 21};
+    for (int axis = 0, pair = 0; axis < r->axes; ++axis) {
+        // base^(-j / n) as powers of one number: off by at most j roundings of 64 bits
+        const double step = pow((double)r->base, -1.0 / counts[axis]);
+        double turns = 1.0 / 6.283185307179586476925;
+        for (int j = 0; j < counts[axis]; ++j, turns *= step) a->turns[pair++] = turns;
+    }
+}
+
+// One kind of rows (q or k) of the norm and rotation.
+const char* turn_rows_wrong(const void* p, int64_t stride, int heads, const float* gain, const void* out, int64_t out_stride, bool has_out) {
+    if (const char* why = rows_wrong(p, stride, (int64_t)heads * SDV2_HEAD_DIM, 2)) return why;
+    if (gain && !aligned16(gain)) return "gain is not 16-byte aligned";
+    if (!has_out) return nullptr;
+    if (const char* why = rows_wrong(out, out_stride, (int64_t)heads * SDV2_HEAD_DIM, 2)) return why;
+    if (out == p && out_stride != stride) return "in place needs the same stride";
+    return nullptr;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t sdv2_paged_pool_bytes(const sdv2_paged_cfg* cfg) {
+    if (const char* why = paged_cfg_wrong(cfg)) {
+        fail(SDV2_INVALID_ARG, "%s", why);
+        return 0;
+    }
+    return (size_t)cfg->n_pages * cfg->kv_heads * cfg->page_tokens * SDV2_HEAD_DIM * (cfg->format == SDV2_PAGES_E4M3 ? 1 : 2);
+}
+
+int32_t sdv2_qk_norm_rope(const sdv2_rope_cfg* rope, int32_t n_tokens, const int32_t* pos_dev,
+                          const void* q_dev, int64_t q_stride, int32_t q_heads, const float* g_q_dev, void* q_out_dev, int64_t q_out_stride,
+                          const void* k_dev, int64_t k_stride, int32_t k_heads, const float* g_k_dev, void* k_out_dev, int64_t k_out_stride,
+                          void* hip_stream) {
+    if (!rope) return fail(SDV2_INVALID_ARG, "rope is null");
+    if (const char* why = rope_wrong(rope)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (n_tokens < 0 || q_heads < 0 || k_heads < 0 || q_heads + (int64_t)k_heads == 0) return fail(SDV2_INVALID_ARG, "bad n_tokens or heads");
+    if ((int64_t)n_tokens * (q_heads + (int64_t)k_heads) > kMostRowHeads) return fail(SDV2_INVALID_ARG, "more than 2^26 heads of rows");
+    if (n_tokens == 0) return SDV2_OK;
+    if (rope->axes > 0 && !pos_dev) return fail(SDV2_INVALID_ARG, "positions are null");
+    if (q_heads > 0)
+        if (const char* why = turn_rows_wrong(q_dev, q_stride, q_heads, g_q_dev, q_out_dev, q_out_stride, true)) return fail(SDV2_INVALID_ARG, "q: %s", why);
+    if (k_heads > 0)
+        if (const char* why = turn_rows_wrong(k_dev, k_stride, k_heads, g_k_dev, k_out_dev, k_out_stride, true)) return fail(SDV2_INVALID_ARG, "k: %s", why);
+    TurnArgs a{};
+    a.q = static_cast<const bf16*>(q_dev);
+    a.k = static_cast<const bf16*>(k_dev);
+    a.q_out = static_cast<bf16*>(q_out_dev);
+    a.k_out = static_cast<bf16*>(k_out_dev);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.q_out_stride = q_out_stride;
+    a.k_out_stride = k_out_stride;
+    a.rows = n_tokens;
+    a.q_heads = q_heads;
+    a.k_heads = k_heads;
+    a.g_q = g_q_dev;
+    a.g_k = g_k_dev;
+    set_rotation(&a, rope, pos_dev);
+    HIP_TRY(launch_turn(a, static_cast<hipStream_t>(hip_stream)), "norm and rotation kernel");
+    return SDV2_OK;
+}
+
+int32_t sdv2_paged_append(const sdv2_paged_cfg* cfg, void* k_pages_dev, void* v_pages_dev, const sdv2_ragged_batch* batch,
+                          const sdv2_rope_cfg* rope, const int32_t* pos_dev,
+                          const void* k_dev, int64_t k_stride, const float* g_k_dev, const void* v_dev, int64_t v_stride,
+                          const void* q_dev, int64_t q_stride, int32_t q_heads, const float* g_q_dev, void* q_out_dev, int64_t q_out_stride,
+                          void* hip_stream) {
+    if (const char* why = paged_cfg_wrong(cfg)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (const char* why = batch_wrong(batch, cfg)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (rope)
+        if (const char* why = rope_wrong(rope)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (!rope && (pos_dev || g_k_dev || g_q_dev)) return fail(SDV2_INVALID_ARG, "gains or positions without rope");
+    if (q_heads < 0) return fail(SDV2_INVALID_ARG, "q_heads < 0");
+    if ((int64_t)batch->n_tokens * (q_heads + 2 * (int64_t)cfg->kv_heads) > kMostRowHeads) return fail(SDV2_INVALID_ARG, "more than 2^26 heads of rows");
+    if (batch->n_tokens == 0) return SDV2_OK;
+    if (const char* why = batch_arrays_wrong(batch)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (rope && rope->axes > 0 && !pos_dev) return fail(SDV2_INVALID_ARG, "positions are null");
+    if (!aligned16(k_pages_dev) || !aligned16(v_pages_dev) || !k_pages_dev || !v_pages_dev) return fail(SDV2_INVALID_ARG, "pages are null or misaligned");
+    if (const char* why = turn_rows_wrong(k_dev, k_stride, cfg->kv_heads, g_k_dev, nullptr, 0, false)) return fail(SDV2_INVALID_ARG, "k: %s", why);
+    if (const char* why = turn_rows_wrong(v_dev, v_stride, cfg->kv_heads, nullptr, nullptr, 0, false)) return fail(SDV2_INVALID_ARG, "v: %s", why);
+    if (q_heads > 0)
+        if (const char* why = turn_rows_wrong(q_dev, q_stride, q_heads, g_q_dev, q_out_dev, q_out_stride, true)) return fail(SDV2_INVALID_ARG, "q: %s", why);
+    TurnArgs a{};
+    a.q = static_cast<const bf16*>(q_dev);
+    a.k = static_cast<const bf16*>(k_dev);
+    a.v = static_cast<const bf16*>(v_dev);
+    a.q_out = static_cast<bf16*>(q_out_dev);
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q_out_stride = q_out_stride;
+    a.rows = batch->n_tokens;
+    a.q_heads = q_heads;
+    a.k_heads = cfg->kv_heads;
+    a.g_q = g_q_dev;
+    a.g_k = g_k_dev;
+    if (rope) set_rotation(&a, rope, pos_dev);
+    a.batch = ragged_args(batch, cfg);
+    a.k_pages = k_pages_dev;
+    a.v_pages = v_pages_dev;
+    a.e4m3 = cfg->format == SDV2_PAGES_E4M3;
+    a.k_inverse = 1.0f / cfg->k_scale;
+    a.v_inverse = 1.0f / cfg->v_scale;
+    HIP_TRY(launch_turn(a, static_cast<hipStream_t>(hip_stream)), "paged append kernel");
+    return SDV2_OK;
+}
+
+static const char* paged_attention_wrong(const sdv2_paged_cfg* cfg, const sdv2_ragged_batch* batch, const sdv2_attn_mask* mask, int32_t q_heads) {
+    if (const char* why = paged_cfg_wrong(cfg)) return why;
+    if (const char* why = batch_wrong(batch, cfg)) return why;
+    if (!mask || mask->struct_size != sizeof(sdv2_attn_mask)) return "mask is null or its struct_size wrong";
+    if (mask->block < 0 || mask->window < 0 || mask->sink < 0) return "negative block, window or sink";
+    if (mask->scale != mask->scale || isinf(mask->scale)) return "scale is not finite";
+    if (q_heads <= 0 || q_heads % cfg->kv_heads) return "q_heads must be a multiple of kv_heads";
+    if ((int64_t)batch->n_tokens * q_heads > kMostRowHeads) return "more than 2^26 heads of rows";
+    return nullptr;
+}
+
+static size_t paged_attention_bytes(const PagedAttnPlan& plan, int64_t row_heads) {
+    return plan.parts > 1 ? (size_t)plan.parts * row_heads * (SDV2_HEAD_DIM + 2) * sizeof(float) : 0;
+}
+
+size_t sdv2_paged_attention_workspace_bytes(const sdv2_paged_cfg* cfg, const sdv2_ragged_batch* batch, const sdv2_attn_mask* mask, int32_t q_heads) {
+    if (const char* why = paged_attention_wrong(cfg, batch, mask, q_heads)) {
+        fail(SDV2_INVALID_ARG, "%s", why);
+        return 0;
+    }
+    const PagedAttnPlan plan = plan_paged_attention(ragged_args(batch, cfg), q_heads, batch->max_q_len, batch->max_kv_len, cfg->format == SDV2_PAGES_E4M3);
+    return paged_attention_bytes(plan, (int64_t)batch->n_tokens * q_heads);
+}
+
+int32_t sdv2_paged_attention(const sdv2_paged_cfg* cfg, const void* k_pages_dev, const void* v_pages_dev, const sdv2_ragged_batch* batch,
+                             const sdv2_attn_mask* mask, const void* q_dev, int64_t q_stride, int32_t q_heads, void* o_dev, int64_t o_stride,
+                             void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    if (const char* why = paged_attention_wrong(cfg, batch, mask, q_heads)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (batch->n_tokens == 0) return SDV2_OK;
+    if (const char* why = batch_arrays_wrong(batch)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (!aligned16(k_pages_dev) || !aligned16(v_pages_dev) || !k_pages_dev || !v_pages_dev) return fail(SDV2_INVALID_ARG, "pages are null or misaligned");
+    const int64_t width = (int64_t)q_heads * SDV2_HEAD_DIM;
+    if (const char* why = rows_wrong(q_dev, q_stride, width, 2)) return fail(SDV2_INVALID_ARG, "q: %s", why);
+    if (const char* why = rows_wrong(o_dev, o_stride, width, 2)) return fail(SDV2_INVALID_ARG, "o: %s", why);
+    PagedAttnArgs a{};
+    a.batch = ragged_args(batch, cfg);
+    const int e4m3 = cfg->format == SDV2_PAGES_E4M3;
+    const PagedAttnPlan plan = plan_paged_attention(a.batch, q_heads, batch->max_q_len, batch->max_kv_len, e4m3);
+    const int64_t row_heads = (int64_t)batch->n_tokens * q_heads;
+    const size_t need = paged_attention_bytes(plan, row_heads);
+    if (need > 0 && (!workspace_dev || workspace_bytes < need)) return fail(SDV2_WORKSPACE_TOO_SMALL, "paged attention workspace %zu < %zu", workspace_bytes, need);
+    if (need > 0 && !aligned16(workspace_dev)) return fail(SDV2_INVALID_ARG, "workspace is not 16-byte aligned");
+    a.mask.block = mask->block;
+    a.mask.window = mask->window;
+    a.mask.sink = mask->sink;
+    const float scale = mask->scale > 0.0f ? mask->scale : 1.0f / sqrtf((float)SDV2_HEAD_DIM);
+    a.mask.scale_log2e = scale * 1.4426950408889634f * cfg->k_scale;
+    a.q = static_cast<const bf16*>(q_dev);
+    a.o = static_cast<bf16*>(o_dev);
+    a.q_stride = q_stride;
+    a.o_stride = o_stride;
+    a.k_pages = k_pages_dev;
+    a.v_pages = v_pages_dev;
+    a.q_heads = q_heads;
+    a.group = q_heads / cfg->kv_heads;
+    a.v_scale = cfg->v_scale;
+    a.parts = plan.parts;
+    a.part_o = static_cast<float*>(workspace_dev);
+    a.part_ml = a.part_o ? a.part_o + (size_t)plan.parts * row_heads * SDV2_HEAD_DIM : nullptr;
+    HIP_TRY(launch_paged_attention(a, plan, e4m3, static_cast<hipStream_t>(hip_stream)), "paged attention kernel");
+    return SDV2_OK;
+}
+
+static const char* lora_wrong(const sdv2_lora_cfg* c) {
+    if (!c || c->struct_size != sizeof(sdv2_lora_cfg)) return "cfg is null or its struct_size wrong";
+    if (c->K <= 0 || c->K % 64 || c->N <= 0 || c->N % 64) return "K and N must be positive multiples of 64";
+    if (c->K > (1 << 20) || c->N > (1 << 20)) return "K or N too large";
+    if (c->rank <= 0 || c->rank % 8 || c->rank > 128) return "rank must be a multiple of 8 up to 128";
+    if (c->n_adapters <= 0) return "n_adapters must be positive";
+    if (c->out_fp32 != 0 && c->out_fp32 != 1) return "out_fp32 must be 0 or 1";
+    if (c->n_seqs <= 0 || c->n_seqs > (1 << 22) || c->n_tokens < 0 || c->n_tokens > (1 << 22) || c->max_q_len < 0) return "n_seqs, n_tokens or max_q_len out of range";
+    return nullptr;
+}
+
+static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)parts * c->n_tokens * c->rank * sizeof(float), 256); }
+
+size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg) {
+    if (const char* why = lora_wrong(cfg)) {
+        fail(SDV2_INVALID_ARG, "%s", why);
+        return 0;
+    }
+    return lora_bytes(cfg, lora_parts(cfg->n_seqs, cfg->n_tokens, cfg->max_q_len, cfg->K, cfg->rank));
+}
+
+int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* b_dev, const float* scale_dev, const int32_t* adapter_dev,
+                       const int32_t* q_start_dev, const void* x_dev, int64_t x_stride, const void* y_dev, int64_t y_stride,
+                       void* out_dev, int64_t out_stride, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+    if (const char* why = lora_wrong(cfg)) return fail(SDV2_INVALID_ARG, "%s", why);
+    if (cfg->n_tokens == 0) return SDV2_OK;
+    if (!a_dev || !b_dev || !adapter_dev || !q_start_dev) return fail(SDV2_INVALID_ARG, "null pointer");
+    if (!aligned16(a_dev) || !aligned16(b_dev)) return fail(SDV2_INVALID_ARG, "adapters are not 16-byte aligned");
+    const int size = cfg->out_fp32 ? 4 : 2;
+    if (const char* why = rows_wrong(x_dev, x_stride, cfg->K, 2)) return fail(SDV2_INVALID_ARG, "x: %s", why);
+    if (const char* why = rows_wrong(y_dev, y_stride, cfg->N, size)) return fail(SDV2_INVALID_ARG, "y: %s", why);
+    if (const char* why = rows_wrong(out_dev, out_stride, cfg->N, size)) return fail(SDV2_INVALID_ARG, "out: %s", why);
+    if (out_dev == y_dev && out_stride != y_stride) return fail(SDV2_INVALID_ARG, "in place needs the same stride");
+    const int parts = lora_parts(cfg->n_seqs, cfg->n_tokens, cfg->max_q_len, cfg->K, cfg->rank);
+    const size_t need = lora_bytes(cfg, parts);
+    if (!workspace_dev || workspace_bytes < need) return fail(SDV2_WORKSPACE_TOO_SMALL, "lora workspace %zu < %zu", workspace_bytes, need);
+    if (!aligned16(workspace_dev)) return fail(SDV2_INVALID_ARG, "workspace is not 16-byte aligned");
+    LoraArgs a{};
+    a.x = static_cast<const bf16*>(x_dev);
+    a.a = static_cast<const bf16*>(a_dev);
+    a.b = static_cast<const bf16*>(b_dev);
+    a.scale = scale_dev;
+    a.adapter = adapter_dev;
+    a.q_start = q_start_dev;
+    a.y = y_dev;
+    a.out = out_dev;
+    a.x_stride = x_stride;
+    a.y_stride = y_stride;
+    a.out_stride = out_stride;
+    a.n_seqs = cfg->n_seqs;
+    a.n_tokens = cfg->n_tokens;
+    a.K = cfg->K;
+    a.N = cfg->N;
+    a.rank = cfg->rank;
+    a.n_adapters = cfg->n_adapters;
+    a.fp32 = cfg->out_fp32;
+    a.u = static_cast<float*>(workspace_dev);
+    a.parts = parts;
+    HIP_TRY(launch_lora(a, static_cast<hipStream_t>(hip_stream)), "adapter kernels");
     return SDV2_OK;
 }
 

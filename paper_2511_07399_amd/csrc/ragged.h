@@ -1,0 +1,126 @@
+// What the kernels of ragged batches share: sequences of different lengths in one list of rows, pages of a cache that a table names.
+#pragma once
+
+#include "common.h"
+
+namespace sdv2 {
+
+// Rows q_start[s] .. q_start[s + 1] - 1 are the new tokens of sequence s, the last of its kv_len[s] tokens; token j lies in page
+// table[s * table_stride + (j >> page_shift)] at slot j & (P - 1).  An entry outside [0, n_pages) names no page.
+struct RaggedArgs {
+    const int* q_start;       // [n_seqs + 1]
+    const int* kv_len;        // [n_seqs]
+    const int* table;         // [n_seqs][table_stride]
+    int n_seqs, n_tokens, table_stride;
+    int page_shift, n_pages, kv_heads;
+};
+
+// Sequence of row t (n_seqs: behind the last one), found by the whole wave: each round 64 lanes look at the ends of 64 runs of
+// sequences at once, so that 64 sequences take one load and 4096 two, one behind the other, where a bisection takes 6 and 12.
+__device__ __forceinline__ int sequence_of_row(const RaggedArgs& b, int t) {
+    const int lane = threadIdx.x & 63;
+    int first = 0, n = b.n_seqs;                             // it is one of first .. first + n, the last meaning "behind"
+    while (n > 0) {
+        const int run = (n + 63) >> 6;                       // sequences per lane
+        const int last = min(first + (lane + 1) * run, first + n);
+        const bool before = first + lane * run < first + n && b.q_start[last] <= t;      // t is behind this lane's run
+        const int runs = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
+        const int left = first + n - min(first + n, first + runs * run);
+        first = min(first + n, first + runs * run);
+        n = run == 1 ? 0 : min(run, left);
+        if (n > 0) --n;                                      // that run's end is behind t, so its last sequence is the last candidate
+    }
+    return __builtin_amdgcn_readfirstlane(first);
+}
+
+// Keys that a row may see: j < end, and j >= low or j < sink.
+struct RowKeys {
+    int end, low, sink;
+};
+struct MaskArgs {
+    int block;                // 0: all keys; B: those of the row's block of B tokens and before
+    int window, sink;         // 0: no window; else the last `window` keys up to the end, and the first `sink`
+    float scale_log2e;        // softmax scale times log2 e (and the keys' scale)
+};
+// Row i of n new tokens of a sequence of kv_len tokens.
+__device__ __forceinline__ RowKeys row_keys(const MaskArgs& m, int i, int n, int kv_len) {
+    const int p = kv_len - n + i;
+    int end = max(kv_len, 0);
+    if (m.block > 0) end = p < 0 ? 0 : (int)min((long long)kv_len, ((long long)(p / m.block) + 1) * m.block);
+    const int low = m.window > 0 ? max(0, end - m.window) : 0;
+    return RowKeys{end, low, m.window > 0 ? min(m.sink, low) : 0};
+}
+
+// Eight bf16 from eight e4m3 (exact).
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16x8 widen_e4m3(u32x2 v) {
+    bf16x8 out;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[w], 1.0f, false);
+        const bf16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v[w], 1.0f, true);
+        out[4 * w] = lo[0];
+        out[4 * w + 1] = lo[1];
+        out[4 * w + 2] = hi[0];
+        out[4 * w + 3] = hi[1];
+    }
+    return out;
+}
+
+// ---------------------------------------------------------------- launchers (host side)
+// Norm of each head and rotation of q and k, out of place or in place, or into pages together with v.
+struct TurnArgs {
+    const bf16 *q, *k, *v;            // rows of heads of 128; q or k may be null (no heads), v is null without pages
+    bf16 *q_out, *k_out;              // k_out is null with pages
+    long long q_stride, k_stride, v_stride, q_out_stride, k_out_stride;     // elements from row to row
+    int rows, q_heads, k_heads;
+    const float *g_q, *g_k;           // gains [128] of the norm; null: no norm
+    float eps;
+    int axes, halves;                 // axes 0: no rotation
+    const int* pos;                   // [rows][axes]
+    double turns[kHeadDim / 2];       // of each pair: revolutions per unit of its axis' position
+    // with pages
+    RaggedArgs batch;
+    void *k_pages, *v_pages;          // [n_pages][kv_heads][P][128] bf16 or e4m3
+    int e4m3;
+    float k_inverse, v_inverse;       // 1 / scale (1 for bf16)
+};
+hipError_t launch_turn(const TurnArgs& a, hipStream_t s);
+
+struct PagedAttnArgs {
+    RaggedArgs batch;
+    MaskArgs mask;
+    const bf16* q;
+    bf16* o;
+    long long q_stride, o_stride;
+    const void *k_pages, *v_pages;
+    int q_heads, group;               // query heads, and those of one key head
+    float v_scale;
+    float* part_o;                    // [parts][n_tokens * q_heads][128]
+    float* part_ml;                   // [parts][n_tokens * q_heads][2]
+    int parts;
+};
+struct PagedAttnPlan {
+    int form, parts;
+};
+PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_len, int max_kv_len, int e4m3);
+hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& plan, int e4m3, hipStream_t s);
+
+struct LoraArgs {
+    const bf16* x;                    // [rows][x_stride], K of them
+    const bf16* a;                    // [n_adapters][rank][K]
+    const bf16* b;                    // [n_adapters][N][rank]
+    const float* scale;               // [n_adapters] or null
+    const int* adapter;               // [n_seqs]
+    const int* q_start;               // [n_seqs + 1]
+    const void* y;
+    void* out;
+    long long x_stride, y_stride, out_stride;
+    int n_seqs, n_tokens, K, N, rank, n_adapters, fp32;
+    float* u;                         // [parts][n_tokens][rank]
+    int parts;
+};
+int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank);
+hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
+
+}  // namespace sdv2
