@@ -2,67 +2,596 @@
 //
 //   o = sum_j p_j v_j / sum_j p_j,  p_j = exp(scale q . k_j) over the keys j that the row may see; the zero row where there is none.
 //
-// One wave per row and query head, a key at a time, with the running maximum and sum of the softmax.
 #include "ragged.h"
+
+#include <mutex>
+#include <type_traits>
 
 namespace sdv2 {
 
 namespace {
 
 constexpr int D = kHeadDim;
+constexpr float kSlack = 8.0f;       // log2 units that a row's scores may run ahead of its exponents' reference point
+constexpr float kNoKey = -1.0e30f;   // reference point of a row that has seen no key yet: finite, so that -inf minus it is -inf
+
+typedef __attribute__((address_space(3))) void* lds_void_ptr;
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2* lds_i32x2_ptr;
+
+__device__ __forceinline__ void load_to_lds(const void* src, void* dst) { __builtin_amdgcn_global_load_lds(src, (lds_void_ptr)dst, 16, 0, 0); }
+
+// The waits count loads, so loads stay where they are written, and reads of what they bring behind the wait.
+__device__ __forceinline__ void hold_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ void reads_done() {
+    hold_order();
+    __builtin_amdgcn_s_waitcnt(0xC07F);          // lgkmcnt(0)
+    hold_order();
+}
+
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ __forceinline__ float max2(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+// Largest of a block's sixteen scores and of the partner lane's (the same row's other sixteen keys); NaN gives way.
+__device__ __forceinline__ float block_max(const f32x16& s) {
+    float m[4];
+#pragma unroll
+    for (int c = 0; c < 4; ++c) m[c] = max2(max3(s[4 * c], s[4 * c + 1], s[4 * c + 2]), s[4 * c + 3]);
+    const float x = max2(max3(m[0], m[1], m[2]), m[3]);
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return max2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// Two groups of four channels of a row as bf16: a lane has channels 4 lh .. + 3 of two blocks of eight; the halves of the wave trade
+// words so that each lane stores eight channels in a row (lanes < 32 the first block, the others the second).
+__device__ __forceinline__ uint4 eight_channels(const bf16x4& lo, const bf16x4& hi) {
+    const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+    const auto x = __builtin_amdgcn_permlane32_swap(a.x, b.x, false, false);
+    const auto y = __builtin_amdgcn_permlane32_swap(a.y, b.y, false, false);
+    return uint4{x[0], y[0], x[1], y[1]};
+}
+
+// ---------------------------------------------------------------------------------------------------
+// What a workgroup works on: a run of rows of one sequence and key head, and a run of the key tiles that they see.  Row r of a sequence is
+// its token r / group under query head r % group of the key head, so all rows share keys and values.
+struct Work {
+    int seq, hk, part;
+    int q0, n, kv_len;        // first row of the sequence in the batch, its new tokens, its tokens
+    int row0, rows;           // first row of this workgroup, and all of the sequence's
+};
+
+// Row tiles are numbered without a table: those of sequence s start at floor(q_start[s] group / tile) + s, which leaves each sequence
+// at least as many numbers as it has tiles.  False: a number that no tile has.
+__device__ __forceinline__ bool locate(const PagedAttnArgs& a, int tile_rows, unsigned logical, Work* w) {
+    const unsigned rest = divide(logical, a.by_tiles), z = divide(rest, a.by_heads);
+    // the last tiles of a causal prompt see the most keys: they go first
+    const int tile = a.row_tiles - 1 - (int)(logical - rest * a.by_tiles.d);
+    w->hk = (int)(rest - z * a.by_heads.d);
+    w->part = (int)z;
+    auto start = [&](int s) { return (int)((long long)a.batch.q_start[s] * a.group / tile_rows) + s; };
+    w->seq = find_sequence(a.batch.n_seqs, tile, start);
+    if (w->seq >= a.batch.n_seqs) return false;
+    w->q0 = __builtin_amdgcn_readfirstlane(a.batch.q_start[w->seq]);
+    w->n = __builtin_amdgcn_readfirstlane(a.batch.q_start[w->seq + 1]) - w->q0;
+    const long long room = (long long)a.batch.table_stride << a.batch.page_shift;
+    w->kv_len = (int)min((long long)__builtin_amdgcn_readfirstlane(a.batch.kv_len[w->seq]), room);
+    if (w->q0 < 0 || w->n < 0 || w->n > a.batch.n_tokens - w->q0) return false;      // not a batch: touch nothing
+    w->rows = w->n * a.group;
+    w->row0 = (tile - (int)((long long)w->q0 * a.group / tile_rows) - w->seq) * tile_rows;
+    return w->row0 < w->rows;
+}
+
+// The key tiles that a run of rows sees, in order: those of the sink, then those from the window on.
+struct Visited {
+    int sink_tiles, skip;     // tile number n is tile n where n < sink_tiles, n + skip from there on
+    int count;
+    int e_first, low_last, sink_first;      // which tiles need no mask: see whole()
+};
+template <int KT>
+__device__ __forceinline__ Visited visited_tiles(const MaskArgs& m, const Work& w, int first_token, int last_token) {
+    const RowKeys a = row_keys(m, first_token, w.n, w.kv_len), b = row_keys(m, last_token, w.n, w.kv_len);
+    Visited v;
+    v.e_first = a.end;
+    v.low_last = b.low;
+    v.sink_first = a.sink;
+    const int low_tile = a.low / KT, end_tile = (int)((unsigned)(b.end + KT - 1) / KT);
+    v.sink_tiles = (a.sink + KT - 1) / KT;
+    v.skip = v.sink_tiles < low_tile ? low_tile - v.sink_tiles : 0;
+    v.count = max(0, end_tile - v.skip);
+    return v;
+}
+__device__ __forceinline__ int tile_of(const Visited& v, int n) { return n < v.sink_tiles ? n : n + v.skip; }
+// Whether every row sees all keys first .. end - 1 (pages aside).
+__device__ __forceinline__ bool whole(const Visited& v, int first, int end) {
+    return end <= v.e_first && (first >= v.low_last || end <= v.sink_first);
+}
+__device__ __forceinline__ bool sees(const RowKeys& k, int j) { return (j < k.end) & ((j >= k.low) | (j < k.sink)); }
+
+// ---------------------------------------------------------------------------------------------------
+// Tiles of keys and values in LDS as they lie in a page, [key][128], a row's 16-byte chunks permuted so that fragment reads spread
+// over the 64 banks.  Format of a row: 256 bytes of bf16 or 128 of e4m3.
+//   K fragment (32 keys x 16 numbers): a lane reads its key's row, 16 bytes at a time; chunk c of row r lies at c ^ (r % 16), e4m3:
+//     c ^ (r / 2 % 8).  Of e4m3, 16 bytes are two steps' numbers: lane half lh of step s has numbers 32 (s / 2) + 16 lh + 8 (s % 2) .. + 7
+//     where bf16 has 16 s + 8 lh .. + 7, and the query's fragments go by the same rule.
+//   V fragment (32 channels x 16 keys) transposed: ds_read_b64_tr hands each of 16 lanes a column of the rows that the 16 lanes
+//     address, four keys of 16 bits or eight of 8 bits, and the rows are picked in the order in which the scores' accumulators hold
+//     the keys (4 lh .. + 3 and 8 + 4 lh .. + 3 of sixteen).  Chunk c of row r lies at c ^ (r % 4) * 4; e4m3: c ^ 2 (r / 2 % 2 + 2 (r / 8 % 2)).
+template <bool E4M3>
+struct Rows {
+    static constexpr int kRow = E4M3 ? 128 : 256;             // bytes
+    static constexpr int kPerLoad = 1024 / kRow;              // rows of a wave load
+    // byte within the rows of load number i that this lane fetches to its place (K, V)
+    static __device__ __forceinline__ int k_source(int lane, int i) {
+        if (E4M3) return (lane >> 3) * 128 + (((lane & 7) ^ (lane >> 4) ^ (4 * (i & 1))) << 4);
+        return (lane >> 4) * 256 + (((lane & 15) ^ (lane >> 4) ^ (4 * (i & 3))) << 4);
+    }
+    static __device__ __forceinline__ int v_source(int lane, int i) {
+        if (E4M3) return (lane >> 3) * 128 + (((lane & 7) ^ (((lane >> 4) & 1) << 1) ^ ((i & 1) << 2)) << 4);
+        return (lane >> 4) * 256 + (((lane & 15) ^ ((lane >> 4) << 2)) << 4);
+    }
+    static __device__ __forceinline__ int v_position(int row, int chunk) {      // byte of a chunk
+        if (E4M3) return row * 128 + ((chunk ^ ((((row >> 1) & 1) | (((row >> 3) & 1) << 1)) << 1)) << 4);
+        return row * 256 + ((chunk ^ ((row & 3) << 2)) << 4);
+    }
+    // first number of this lane's eight in step s of the query
+    static __device__ __forceinline__ int q_number(int s, int lh) { return E4M3 ? 32 * (s >> 1) + 16 * lh + 8 * (s & 1) : 16 * s + 8 * lh; }
+    // the eight fragments of 32 keys
+    static __device__ __forceinline__ void k_fragments(bf16x8 (&f)[8], const unsigned char* tile, int l31, int lh) {
+        if (E4M3) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const uint4 x = *reinterpret_cast<const uint4*>(tile + l31 * 128 + (((2 * s + lh) ^ ((l31 >> 1) & 7)) << 4));
+                f[2 * s] = widen_e4m3(u32x2{x.x, x.y});
+                f[2 * s + 1] = widen_e4m3(u32x2{x.z, x.w});
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 8; ++s) f[s] = *reinterpret_cast<const bf16x8*>(tile + l31 * 256 + (((2 * s + lh) ^ (l31 & 15)) << 4));
+        }
+    }
+    // this lane's byte of the reads of channels 32 db .. + 31 of the first sixteen keys
+    static __device__ __forceinline__ int v_lane(int lane, int db) {
+        const int lh = lane >> 5;
+        if (E4M3) {
+            const int j = (lane & 15) >> 1, g = ((j >> 1) & 1) | ((j >> 2) << 1);
+            return (4 * lh + (j & 3) + 8 * (j >> 2)) * 128 + ((db ^ g) << 5) + ((lane >> 4) & 1) * 16 + (lane & 1) * 8;
+        }
+        const int x = (lane >> 2) & 3;
+        return (4 * lh + x) * 256 + ((db ^ x) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    }
+    // fragment of sixteen keys whose rows start at `tile`
+    static __device__ __forceinline__ bf16x8 v_fragment(const unsigned char* tile, int at) {
+        if (E4M3) {
+            const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_ptr)(tile + at));
+            return widen_e4m3(__builtin_bit_cast(u32x2, x));
+        }
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(tile + at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(tile + at + 8 * 256));
+        typedef short s16x8 __attribute__((ext_vector_type(8)));
+        return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // whether these sixteen bytes of values hold an infinity or NaN
+    static __device__ __forceinline__ bool broken(uint4 x) {
+        unsigned hit = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
+            if (E4M3) hit |= ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;                    // 0x7f or 0xff
+            else hit |= ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;                         // exponent of ones
+        }
+        return hit != 0;
+    }
+};
+
+// Bit j: key j of the 32 whose value rows start at row `first` of the tile holds an infinity or NaN.
+template <bool E4M3>
+__device__ __forceinline__ unsigned broken_keys(const unsigned char* v, int first, int lane) {
+    typedef Rows<E4M3> R;
+    const int row = first + (lane & 31);
+    bool hit = false;
+    constexpr int kChunks = R::kRow / 16 / 2;                 // of this lane: half a row
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        // each lane starts at another chunk, so that the lanes of a read do not all hit one bank
+        const int chunk = (lane >> 5) * kChunks + ((c + lane) & (kChunks - 1));
+        hit |= R::broken(*reinterpret_cast<const uint4*>(v + R::v_position(row, chunk)));
+    }
+    const unsigned long long b = __builtin_amdgcn_ballot_w64(hit);
+    return (unsigned)(b | (b >> 32));
+}
+
+// O^T += V^T P^T of 32 keys (rows `first` .. of the value tile) of which `broken` hold infinities or NaN: those leave the products, where
+// zero times them would reach rows that do not see the key, and are added one by one to the rows that do.  Rare, so short, not fast.
+template <bool E4M3>
+__device__ __forceinline__ void add_values_apart(f32x16 (&o)[4], const unsigned char* v, int first, const f32x16& p, unsigned broken, int lane) {
+    typedef Rows<E4M3> R;
+    const int lh = lane >> 5;
+#pragma unroll
+    for (int ts = 0; ts < 2; ++ts) {
+        bf16x8 pf;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) pf[e] = (bf16)p[8 * ts + e];
+#pragma unroll
+        for (int db = 0; db < 4; ++db) {
+            bf16x8 vf = R::v_fragment(v + (first + 16 * ts) * R::kRow, R::v_lane(lane, db));
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if ((broken >> (16 * ts + 4 * lh + (e & 3) + 8 * (e >> 2))) & 1) vf[e] = (bf16)0.0f;
+            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[db], 0, 0, 0);
+        }
+    }
+    for (int j = 0; j < 32; ++j) {
+        if (!((broken >> j) & 1)) continue;
+        float own = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (r == 4 * (j >> 3) + (j & 3)) own = p[r];
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(own), __float_as_uint(own), false, false);
+        const float pj = __uint_as_float((j >> 2) & 1 ? both[1] : both[0]);
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int d = 32 * db + 8 * g + 4 * lh + e;
+                    float x;
+                    if (E4M3) {
+                        const unsigned b = v[R::v_position(first + j, d >> 4) + (d & 15)];
+                        x = (float)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false)[0];
+                    } else {
+                        x = (float)*reinterpret_cast<const bf16*>(v + R::v_position(first + j, d >> 3) + (d & 7) * 2);
+                    }
+                    if (pj != 0.0f) o[db][4 * g + e] += pj * x;
+                }
+    }
+}
+
+// Output of a lane's row: 32 NDB channels from d0 on, value(db, g, e) = channel d0 + 32 db + 8 g + 4 lh + e before the division by the
+// sum.  Whole key range: bf16 to o.  In parts: 32 bits and (m, l) to the workspace, for the join.
+template <int NDB, typename F>
+__device__ __forceinline__ void store_rows(const PagedAttnArgs& a, const Work& w, bool live, int token, int head, float m, float l, int d0,
+                                           bool write_ml, int lh, F&& value) {
+    const int t = w.q0 + token;
+    if (a.parts == 1) {
+        const float inv = l != 0.0f ? a.v_scale / l : 0.0f;
+        bf16* const op = a.o + t * a.o_stride + head * D + d0 + 8 * lh;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+            for (int g = 0; g < 4; g += 2) {
+                bf16x4 x[2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[0][e] = (bf16)(value(db, g, e) * inv);
+                    x[1][e] = (bf16)(value(db, g + 1, e) * inv);
+                }
+                const uint4 v = eight_channels(x[0], x[1]);
+                if (live) *reinterpret_cast<uint4*>(op + 32 * db + 8 * g) = v;
+            }
+        return;
+    }
+    if (!live) return;
+    const long long at = ((long long)w.part * a.batch.n_tokens + t) * a.q_heads + head;
+    float* const op = a.part_o + at * D + d0 + 4 * lh;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = value(db, g, e);
+            *reinterpret_cast<f32x4*>(op + 32 * db + 8 * g) = x;
+        }
+    if (write_ml) {
+        a.part_ml[at * 2] = m;
+        a.part_ml[at * 2 + 1] = l;
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Few rows: the keys are what is read, and the memory what bounds it.  A workgroup has at most 32 rows; its four waves take the key
+// tiles of 32 in turn, each with a buffer of its own in LDS that direct loads fill and no barrier guards: a wave waits for its own loads
+// only, and fetches the next keys as soon as its fragments of these are in registers.  Two workgroups per compute unit, up to 128 KB of
+// loads on their way.  The waves' outputs are joined through LDS, those of the key range's parts by a second launch.
+constexpr int kTokenTile = 32, kTokenWaves = 4;
 
 template <bool E4M3>
-__global__ __launch_bounds__(256) void paged_attention_row_kernel(PagedAttnArgs a) {
-    const int lane = threadIdx.x & 63;
-    const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t = __builtin_amdgcn_readfirstlane((int)(wave / a.q_heads)), h = __builtin_amdgcn_readfirstlane((int)(wave % a.q_heads));
-    if (t >= a.batch.n_tokens) return;
-    const int s = sequence_of_row(a.batch, t);
-    if (s >= a.batch.n_seqs) return;
-    const int q0 = a.batch.q_start[s], n = a.batch.q_start[s + 1] - q0;
-    const int kv_len = (int)min((long long)a.batch.kv_len[s], (long long)a.batch.table_stride << a.batch.page_shift);
-    const RowKeys keys = row_keys(a.mask, t - q0, n, kv_len);
-    const int hk = h / a.group;
-    const bf16x2 q = *reinterpret_cast<const bf16x2*>(a.q + t * a.q_stride + h * D + lane * 2);
-    float m = -INFINITY, l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    for (int j = 0; j < keys.end; ++j) {
-        if (j >= keys.sink && j < keys.low) j = keys.low;
-        const int page = a.batch.table[(long long)s * a.batch.table_stride + (j >> a.batch.page_shift)];
-        if ((unsigned)page >= (unsigned)a.batch.n_pages) continue;
-        const long long at =
-            ((((long long)page * a.batch.kv_heads + hk) << a.batch.page_shift) + (j & ((1 << a.batch.page_shift) - 1))) * D + lane * 2;
-        float k0, k1, v0, v1;
-        if (E4M3) {
-            const bf16x2 k = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(*reinterpret_cast<const unsigned short*>(static_cast<const unsigned char*>(a.k_pages) + at), 1.0f, false);
-            const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(*reinterpret_cast<const unsigned short*>(static_cast<const unsigned char*>(a.v_pages) + at), 1.0f, false);
-            k0 = (float)k[0], k1 = (float)k[1], v0 = (float)v[0], v1 = (float)v[1];
-        } else {
-            const bf16x2 k = *reinterpret_cast<const bf16x2*>(static_cast<const bf16*>(a.k_pages) + at);
-            const bf16x2 v = *reinterpret_cast<const bf16x2*>(static_cast<const bf16*>(a.v_pages) + at);
-            k0 = (float)k[0], k1 = (float)k[1], v0 = (float)v[0], v1 = (float)v[1];
-        }
-        const float x = wave_sum((float)q[0] * k0 + (float)q[1] * k1) * a.mask.scale_log2e;
-        const float top = fmaxf(m, x);
-        const float keep = m == top ? 1.0f : __builtin_amdgcn_exp2f(m - top), p = __builtin_amdgcn_exp2f(x - top);
-        l = l * keep + p;
-        o0 = o0 * keep + p * v0;
-        o1 = o1 * keep + p * v1;
-        m = top;
+__global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAttnArgs a) {
+    typedef Rows<E4M3> R;
+    constexpr int KT = kTokenTile, NW = kTokenWaves;
+    constexpr int kStages = E4M3 ? 2 : 1;
+    constexpr int kTile = KT * R::kRow, kLoads = KT / R::kPerLoad;          // bytes and wave loads of a K or V tile
+    static_assert(NW * kStages * 2 * kTile == 65536, "the launch's LDS, which the waves' outputs fill too");
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    unsigned char* const k_first = smem;
+    unsigned char* const v_first = smem + NW * kTile;
+    unsigned char* const k_second = smem + 2 * NW * kTile;
+    unsigned char* const v_second = smem + 3 * NW * kTile;
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l31 = lane & 31, lh = lane >> 5;
+    Work w;
+    if (!locate(a, KT, blockIdx.x, &w)) return;
+    const int last_row = min(w.row0 + 32, w.rows) - 1;
+    const Visited vis = visited_tiles<KT>(a.mask, w, w.row0 / a.group, last_row / a.group);
+    const int first = min(vis.count, w.part * a.part_tiles), end = w.part == a.parts - 1 ? vis.count : min(vis.count, first + a.part_tiles);
+    if (w.part > 0 && first >= end) return;                                  // nobody reads this part
+    const int count = max(0, (end - first - wave + NW - 1) / NW);           // tiles of this wave
+
+    // this lane's row
+    const int row = min(w.row0 + l31, w.rows - 1), token = (int)divide(row, a.by_group), head = w.hk * a.group + row - token * a.group;
+    const bool live = w.row0 + l31 < w.rows;
+    const RowKeys keys = row_keys(a.mask, token, w.n, w.kv_len);
+    bf16x8 qf[8];
+    {
+        const bf16* qp = a.q + (long long)(w.q0 + token) * a.q_stride + head * D;
+#pragma unroll
+        for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(qp + R::q_number(s, lh));
     }
-    const float inv = l != 0.0f ? a.v_scale / l : 0.0f;
-    *reinterpret_cast<bf16x2*>(a.o + t * a.o_stride + h * D + lane * 2) = bf16x2{(bf16)(o0 * inv), (bf16)(o1 * inv)};
+
+    const int* const table = a.batch.table + (long long)w.seq * a.batch.table_stride;
+    const int slot_mask = (1 << a.batch.page_shift) - 1;
+
+    f32x16 o[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = 0.0f;
+    float m = kNoKey, l = 0.0f;
+
+    // 32 tiles at a time, whose 64 pages of sixteen keys the lanes look up together
+    for (int batch = 0; batch < count; batch += 32) {
+        const int n = min(32, count - batch);
+        int pages;
+        {
+            const int t = tile_of(vis, first + wave + NW * (batch + min(lane >> 1, n - 1)));
+            pages = table[min((t * KT + 16 * (lane & 1)) >> a.batch.page_shift, a.batch.table_stride - 1)];
+        }
+        const bool gone = (unsigned)pages >= (unsigned)a.batch.n_pages;
+        const unsigned long long holes = __builtin_amdgcn_ballot_w64(gone);
+        if (gone) pages = 0;                                                 // fetched, not seen
+        auto fetch = [&](const void* pool, int i, unsigned char* to, bool values) {
+            const int t = tile_of(vis, first + wave + NW * (batch + i));
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const long long page = __builtin_amdgcn_readlane(pages, 2 * i + half);
+                const unsigned char* src = static_cast<const unsigned char*>(pool) +
+                    (((page * a.batch.kv_heads + w.hk) << a.batch.page_shift) + ((t * KT + 16 * half) & slot_mask)) * R::kRow;
+#pragma unroll
+                for (int x = 0; x < kLoads / 2; ++x) {
+                    const int load = half * (kLoads / 2) + x;
+                    load_to_lds(src + x * 1024 + (values ? R::v_source(lane, load) : R::k_source(lane, load)), to + load * 1024);
+                }
+            }
+        };
+        // (restrict: a transposing read is taken to wait for every load on its way to LDS that may alias it)
+        auto step = [&](unsigned char* __restrict__ kt, unsigned char* __restrict__ vt, int i) __attribute__((always_inline)) {
+            const int t = tile_of(vis, first + wave + NW * (batch + i)), key0 = t * KT;
+            // these keys are there when no more loads are on their way than went out behind theirs
+            if (i + kStages - 1 < n) __builtin_amdgcn_s_waitcnt(0x0F70 | (kLoads * (2 * kStages - 1)));
+            else __builtin_amdgcn_s_waitcnt(0x0F70);
+            hold_order();
+            f32x16 s0, s1;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s0[r] = s1[r] = 0.0f;
+            {
+                bf16x8 kf[8];
+                R::k_fragments(kf, kt, l31, lh);
+#pragma unroll
+                for (int s = 0; s < 8; s += 2) {
+                    s0 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s], qf[s], s0, 0, 0, 0);
+                    s1 = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s + 1], qf[s + 1], s1, 0, 0, 0);
+                }
+            }
+            if (i + kStages < n) {
+                reads_done();                                                // the fragments are in registers
+                fetch(a.k_pages, i + kStages, kt, false);
+            }
+            s0 += s1;
+            const unsigned gaps = (unsigned)(holes >> (2 * i)) & 3u;
+            const bool masked = gaps != 0 || !whole(vis, key0, key0 + KT);
+            if (masked) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int j = 8 * (r >> 2) + 4 * lh + (r & 3);
+                    if (!sees(keys, key0 + j) | (((gaps >> (r >> 3)) & 1) != 0)) s0[r] = -INFINITY;
+                }
+            }
+            const float top = block_max(s0) * a.mask.scale_log2e;
+            if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
+                const bool moved = top > m + kSlack;
+                const float alpha = moved ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+                m = moved ? top : m;
+                l *= alpha;
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+            }
+            float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s0[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[r], a.mask.scale_log2e, -m));
+                sum[r & 3] += s0[r];
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            // and these values: behind them went out kStages - 1 tiles and the keys just asked for
+            if (i + kStages < n) __builtin_amdgcn_s_waitcnt(0x0F70 | (kLoads * (2 * kStages - 1)));
+            else __builtin_amdgcn_s_waitcnt(0x0F70);
+            hold_order();
+            const unsigned broken = masked ? broken_keys<E4M3>(vt, 0, lane) : 0u;
+            if (__builtin_expect(broken != 0, 0)) {
+                add_values_apart<E4M3>(o, vt, 0, s0, broken, lane);
+            } else {
+#pragma unroll
+                for (int ts = 0; ts < 2; ++ts) {
+                    bf16x8 pf;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) pf[e] = (bf16)s0[8 * ts + e];
+#pragma unroll
+                    for (int db = 0; db < 4; ++db)
+                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(R::v_fragment(vt + 16 * ts * R::kRow, R::v_lane(lane, db)), pf, o[db], 0, 0, 0);
+                }
+            }
+            if (i + kStages < n) {
+                reads_done();
+                fetch(a.v_pages, i + kStages, vt, true);
+                hold_order();
+            }
+        };
+        fetch(a.k_pages, 0, k_first + wave * kTile, false);
+        hold_order();
+        fetch(a.v_pages, 0, v_first + wave * kTile, true);
+        hold_order();
+        if (kStages == 2 && n > 1) {
+            fetch(a.k_pages, 1, k_second + wave * kTile, false);
+            hold_order();
+            fetch(a.v_pages, 1, v_second + wave * kTile, true);
+            hold_order();
+        }
+        for (int i = 0; i < n; ++i) {
+            step(k_first + wave * kTile, v_first + wave * kTile, i);
+            if (kStages == 2 && ++i < n) step(k_second + wave * kTile, v_second + wave * kTile, i);
+        }
+        reads_done();                                                        // the buffers are free for the next 32 tiles
+    }
+
+    // ---- join the waves, in their order: wave w adds up and stores channels 32 w .. + 31
+    {
+        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+        l = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    }
+    // where a wave's four channels of one kind lie: [wave][4][64] of block db
+    auto place = [&](int wv, int db, int g) {
+        unsigned char* const part = kStages == 2 ? (db == 0 ? k_first : db == 1 ? k_second : db == 2 ? v_first : v_second)
+                                                 : (db < 2 ? k_first : v_first) + (db & 1) * (NW * 4096);
+        return reinterpret_cast<f32x4*>(part) + (wv * 4 + g) * 64 + lane;
+    };
+    __syncthreads();                                                         // everyone is done with the buffers
+    float* const ml = reinterpret_cast<float*>(k_first);                     // [NW][2][32]
+    if (lh == 0) {
+        ml[wave * 64 + l31] = m;
+        ml[wave * 64 + 32 + l31] = l;
+    }
+    __syncthreads();
+    float top = kNoKey, total = 0.0f;
+#pragma unroll
+    for (int k = 0; k < NW; ++k) top = fmaxf(top, ml[k * 64 + l31]);
+#pragma unroll
+    for (int k = 0; k < NW; ++k) total += ml[k * 64 + 32 + l31] * __builtin_amdgcn_exp2f(ml[k * 64 + l31] - top);
+    const float weight = __builtin_amdgcn_exp2f(m - top);
+    __syncthreads();
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            f32x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = o[db][4 * g + e] * weight;
+            *place(wave, db, g) = x;
+        }
+    __syncthreads();
+    f32x4 mine[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        mine[g] = *place(0, wave, g);
+#pragma unroll
+        for (int k = 1; k < NW; ++k) mine[g] += *place(k, wave, g);
+    }
+    store_rows<1>(a, w, live, token, head, top, total, 32 * wave, wave == 0 && lh == 0, lh, [&](int, int g, int e) { return mine[g][e]; });
+}
+
+// Second launch where the key range is in parts: out = sum_i 2^(m_i - max m) O_i / sum_i 2^(m_i - max m) l_i over the parts that the row's
+// workgroup had.  Sixteen lanes a row and head, eight channels each.
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs a, int tile_rows, int key_tile) {
+    const long long row_heads = (long long)a.batch.n_tokens * a.q_heads;
+    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
+    const int c = threadIdx.x & 15;
+    const int t = (int)(min(at, row_heads - 1) / a.q_heads), h = (int)(min(at, row_heads - 1) - (long long)t * a.q_heads);
+    // the sequence, row by row: lanes of a wave may be of several
+    int lo = 0, hi = a.batch.n_seqs;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (a.batch.q_start[mid + 1] <= t) lo = mid + 1;
+        else hi = mid;
+    }
+    if (at >= row_heads || lo >= a.batch.n_seqs) return;
+    Work w;
+    w.q0 = a.batch.q_start[lo];
+    w.n = a.batch.q_start[lo + 1] - w.q0;
+    w.kv_len = (int)min((long long)a.batch.kv_len[lo], (long long)a.batch.table_stride << a.batch.page_shift);
+    if (w.q0 < 0 || t < w.q0 || w.n > a.batch.n_tokens - w.q0) return;
+    // the workgroup that had this row, and so how many parts its keys were in
+    const int row = (t - w.q0) * a.group + h % a.group, row0 = row / tile_rows * tile_rows, last = min(row0 + tile_rows, w.n * a.group) - 1;
+    const int count = key_tile == 32 ? visited_tiles<32>(a.mask, w, row0 / a.group, last / a.group).count
+                                     : visited_tiles<64>(a.mask, w, row0 / a.group, last / a.group).count;
+    const int parts = min(a.parts, max(1, (count + a.part_tiles - 1) / a.part_tiles));
+    float top = kNoKey;
+    for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[(p * row_heads + at) * 2]);
+    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}, total = 0.0f;
+    for (int p = 0; p < parts; ++p) {
+        const float* ml = a.part_ml + (p * row_heads + at) * 2;
+        const float weight = __builtin_amdgcn_exp2f(ml[0] - top);
+        total += weight * ml[1];
+        const f32x4* op = reinterpret_cast<const f32x4*>(a.part_o + (p * row_heads + at) * D + c * 8);
+        const f32x4 x = op[0], y = op[1];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += weight * (e < 4 ? x[e & 3] : y[e & 3]);
+    }
+    const float inv = total != 0.0f ? a.v_scale / total : 0.0f;
+    bf16x8 out;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = (bf16)(acc[e] * inv);
+    *reinterpret_cast<bf16x8*>(a.o + t * a.o_stride + h * D + c * 8) = out;
 }
 
 }  // namespace
 
-PagedAttnPlan plan_paged_attention(const RaggedArgs&, int, int, int, int) { return PagedAttnPlan{0, 1}; }
+PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_len, int max_kv_len, int e4m3) {
+    PagedAttnPlan p{32, 1, 1};
+    const int group = q_heads / b.kv_heads;
+    const long long wgs = ((long long)b.n_tokens * group / 32 + b.n_seqs) * b.kv_heads;
+    const int tiles = (max_kv_len + 31) / 32;
+    int parts = (int)min((long long)(tiles + 15) / 16, (1024 + wgs - 1) / wgs);
+    if (parts < 1) parts = 1;
+    p.part_tiles = max(1, (tiles + parts - 1) / parts);
+    p.parts = max(1, (tiles + p.part_tiles - 1) / p.part_tiles);
+    return p;
+}
 
-hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan&, int e4m3, hipStream_t s) {
-    const long long waves = (long long)a.batch.n_tokens * a.q_heads;
-    const dim3 grid((unsigned)((waves + 3) / 4));
-    if (e4m3) hipLaunchKernelGGL(paged_attention_row_kernel<true>, grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL(paged_attention_row_kernel<false>, grid, dim3(256), 0, s, a);
-    return hipGetLastError();
+hipError_t launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan, int e4m3, hipStream_t s) {
+    PagedAttnArgs a = args;
+    a.parts = plan.parts;
+    a.part_tiles = plan.part_tiles;
+    a.row_tiles = (int)((long long)a.batch.n_tokens * a.group / plan.rows) + a.batch.n_seqs;
+    const long long n_wg = (long long)a.row_tiles * a.batch.kv_heads * plan.parts;
+    a.n_wg = (unsigned)n_wg;
+    a.by_tiles = fast_div((unsigned)a.row_tiles, (unsigned long long)n_wg);
+    a.by_heads = fast_div((unsigned)a.batch.kv_heads, (unsigned long long)n_wg);
+    a.by_group = fast_div((unsigned)a.group, (unsigned long long)a.batch.n_tokens * a.group);
+    if (e4m3) hipLaunchKernelGGL(paged_attention_tokens_kernel<true>, dim3(a.n_wg), dim3(256), 65536, s, a);
+    else hipLaunchKernelGGL(paged_attention_tokens_kernel<false>, dim3(a.n_wg), dim3(256), 65536, s, a);
+    hipError_t e = hipGetLastError();
+    if (e == hipSuccess && plan.parts > 1) {
+        const long long row_heads = (long long)a.batch.n_tokens * a.q_heads;
+        hipLaunchKernelGGL(paged_attention_join_kernel, dim3((unsigned)((row_heads + 15) / 16)), dim3(256), 0, s, a, plan.rows, plan.rows == 32 ? 32 : 64);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 }  // namespace sdv2

@@ -15,22 +15,25 @@ struct RaggedArgs {
     int page_shift, n_pages, kv_heads;
 };
 
-// Sequence of row t (n_seqs: behind the last one), found by the whole wave: each round 64 lanes look at the ends of 64 runs of
-// sequences at once, so that 64 sequences take one load and 4096 two, one behind the other, where a bisection takes 6 and 12.
-__device__ __forceinline__ int sequence_of_row(const RaggedArgs& b, int t) {
+// First of n_seqs sequences whose end, ends(s + 1), is behind t (n_seqs: none), found by the whole wave; ends ascends.  Each round 64
+// lanes look at the ends of 64 runs of sequences at once, so that 64 sequences take one load and 4096 two, one behind the other,
+// where a bisection takes 6 and 12.
+template <typename F>
+__device__ __forceinline__ int find_sequence(int n_seqs, int t, F&& ends) {
     const int lane = threadIdx.x & 63;
-    int first = 0, n = b.n_seqs;                             // it is one of first .. first + n, the last meaning "behind"
+    int first = 0, n = n_seqs;                               // it is one of first .. first + n, the last meaning "behind these"
     while (n > 0) {
-        const int run = (n + 63) >> 6;                       // sequences per lane
-        const int last = min(first + (lane + 1) * run, first + n);
-        const bool before = first + lane * run < first + n && b.q_start[last] <= t;      // t is behind this lane's run
-        const int runs = __builtin_popcountll(__builtin_amdgcn_ballot_w64(before));
-        const int left = first + n - min(first + n, first + runs * run);
-        first = min(first + n, first + runs * run);
-        n = run == 1 ? 0 : min(run, left);
-        if (n > 0) --n;                                      // that run's end is behind t, so its last sequence is the last candidate
+        const int run = (n + 63) >> 6, behind = first + n;   // sequences per lane
+        const int end = min(first + (lane + 1) * run, behind);
+        const bool before = first + lane * run < behind && ends(end) <= t;        // t is behind this lane's run
+        first = min(behind, first + __builtin_popcountll(__builtin_amdgcn_ballot_w64(before)) * run);
+        n = run == 1 ? 0 : min(run, behind - first);
+        if (n > 0) --n;                                      // that run's end is behind t: its last sequence needs no look
     }
     return __builtin_amdgcn_readfirstlane(first);
+}
+__device__ __forceinline__ int sequence_of_row(const RaggedArgs& b, int t) {
+    return find_sequence(b.n_seqs, t, [&](int s) { return b.q_start[s]; });
 }
 
 // Keys that a row may see: j < end, and j >= low or j < sink.
@@ -98,10 +101,14 @@ struct PagedAttnArgs {
     float v_scale;
     float* part_o;                    // [parts][n_tokens * q_heads][128]
     float* part_ml;                   // [parts][n_tokens * q_heads][2]
-    int parts;
+    int parts, part_tiles;            // key tiles of a part; the last part takes what is left
+    FastDiv by_group, by_tiles, by_heads;     // set by the launcher, as is the number of row tiles
+    int row_tiles;
+    unsigned n_wg;
 };
 struct PagedAttnPlan {
-    int form, parts;
+    int rows;                         // rows (tokens times group) of a workgroup: 32, keys over its waves; 128 or 256, rows over its waves
+    int parts, part_tiles;
 };
 PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_len, int max_kv_len, int e4m3);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& plan, int e4m3, hipStream_t s);
