@@ -606,7 +606,8 @@ def prof_gemm_plan(M, N, K, epilogue=0, products=1, workspace_bytes=0):
 
 
 def tuning_set(name, value=None):
-    """Test / sweep hook: force a kernel plan ("gemm_tile", "attn_waves", "attn_splits"); None clears it."""
+    """Test / sweep hook: force a kernel plan ("gemm_tile", "attn_waves", "attn_splits", "paged_rows",
+    "paged_parts"); None clears it."""
     load_library()
     _check(_lib.sdv2_tuning_set(name.encode(), None if value is None else str(value).encode()))
 

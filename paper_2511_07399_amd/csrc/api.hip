@@ -176,6 +176,18 @@ int32_t sdv2_tuning_set(const char* name, const char* value) {
         }
         return SDV2_OK;
     }
+    if (!strcmp(name, "paged_rows")) {
+        const int v = clear ? 0 : atoi(value);
+        if (v != 0 && v != 32 && v != 128 && v != 256) return fail(SDV2_INVALID_ARG, "paged_rows must be 32, 128 or 256");
+        set_paged_overrides(v, -1);
+        return SDV2_OK;
+    }
+    if (!strcmp(name, "paged_parts")) {
+        const int v = clear ? 0 : atoi(value);
+        if (v < 0 || v > 64 || (!clear && v == 0)) return fail(SDV2_INVALID_ARG, "paged_parts must be 1 to 64");
+        set_paged_overrides(-1, v);
+        return SDV2_OK;
+    }
     if (!strcmp(name, "fetch_ahead")) {
         if (!clear && strcmp(value, "0")) return fail(SDV2_INVALID_ARG, "fetch_ahead must be \"0\" or cleared");
         g_fetch_nothing = !clear;

@@ -13,6 +13,7 @@ namespace {
 
 constexpr int D = kHeadDim;
 constexpr float kSlack = 8.0f;       // log2 units that a row's scores may run ahead of its exponents' reference point
+constexpr float kSumLimit = 16384.0f;     // a lane's sum of p over one tile (at most 32 keys) beyond this: move the reference
 constexpr float kNoKey = -1.0e30f;   // reference point of a row that has seen no key yet: finite, so that -inf minus it is -inf
 
 typedef __attribute__((address_space(3))) void* lds_void_ptr;
@@ -213,50 +214,37 @@ __device__ __forceinline__ unsigned broken_keys(const unsigned char* v, int firs
     return (unsigned)(b | (b >> 32));
 }
 
-// O^T += V^T P^T of 32 keys (rows `first` .. of the value tile) of which `broken` hold infinities or NaN: those leave the products, where
-// zero times them would reach rows that do not see the key, and are added one by one to the rows that do.  Rare, so short, not fast.
+// Adds to O^T the keys in `broken` of 32 (rows `first` .. of the value tile), one by one and only to the rows whose p is not zero: in a product
+// with the others, zero times their infinities or NaN would reach rows that do not see them.  pf: the 32 keys' two fragments of p.
+// scratch: 2 KB of the wave's.  The caller then blanks these keys' values and goes on as ever.  Rare, so short, not fast.
+constexpr int kApartBytes = 2048;
 template <bool E4M3>
-__device__ __forceinline__ void add_values_apart(f32x16 (&o)[4], const unsigned char* v, int first, const f32x16& p, unsigned broken, int lane) {
+__device__ __forceinline__ void add_apart(f32x16 (&o)[4], const unsigned char* v, int first, const bf16x8& p0, const bf16x8& p1, unsigned broken,
+                                          unsigned char* scratch, int lane) {
     typedef Rows<E4M3> R;
     const int lh = lane >> 5;
-#pragma unroll
-    for (int ts = 0; ts < 2; ++ts) {
-        bf16x8 pf;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) pf[e] = (bf16)p[8 * ts + e];
-#pragma unroll
-        for (int db = 0; db < 4; ++db) {
-            bf16x8 vf = R::v_fragment(v + (first + 16 * ts) * R::kRow, R::v_lane(lane, db));
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if ((broken >> (16 * ts + 4 * lh + (e & 3) + 8 * (e >> 2))) & 1) vf[e] = (bf16)0.0f;
-            o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, o[db], 0, 0, 0);
-        }
-    }
-    for (int j = 0; j < 32; ++j) {
-        if (!((broken >> j) & 1)) continue;
-        float own = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-            if (r == 4 * (j >> 3) + (j & 3)) own = p[r];
-        const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(own), __float_as_uint(own), false, false);
-        const float pj = __uint_as_float((j >> 2) & 1 ? both[1] : both[0]);
+    *reinterpret_cast<bf16x8*>(scratch + lane * 32) = p0;
+    *reinterpret_cast<bf16x8*>(scratch + lane * 32 + 16) = p1;
+    while (broken != 0) {
+        const int j = __builtin_ctz(broken), row = first + j;
+        broken &= broken - 1;
+        // key j of sixteen: element (j & 3) + 4 (j / 8 % 2) of lane half j / 4 % 2
+        const float p = (float)*reinterpret_cast<const bf16*>(scratch + ((lane & 31) + 32 * ((j >> 2) & 1)) * 32 + (j >> 4) * 16 + ((j & 3) + 4 * ((j >> 3) & 1)) * 2);
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int d = 32 * db + 8 * g + 4 * lh + e;
-                    float x;
-                    if (E4M3) {
-                        const unsigned b = v[R::v_position(first + j, d >> 4) + (d & 15)];
-                        x = (float)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false)[0];
-                    } else {
-                        x = (float)*reinterpret_cast<const bf16*>(v + R::v_position(first + j, d >> 3) + (d & 7) * 2);
-                    }
-                    if (pj != 0.0f) o[db][4 * g + e] += pj * x;
+            for (int g = 0; g < 4; ++g) {
+                bf16x4 x;
+                if (E4M3) {
+                    const unsigned w = *reinterpret_cast<const unsigned*>(v + R::v_position(row, 2 * db + (g >> 1)) + 8 * (g & 1) + 4 * lh);
+                    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+                    x = bf16x4{lo[0], lo[1], hi[0], hi[1]};
+                } else {
+                    x = *reinterpret_cast<const bf16x4*>(v + R::v_position(row, 4 * db + g) + 8 * lh);
                 }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[db][4 * g + e] += p != 0.0f ? p * (float)x[e] : 0.0f;
+            }
     }
 }
 
@@ -308,6 +296,7 @@ __device__ __forceinline__ void store_rows(const PagedAttnArgs& a, const Work& w
 // only, and fetches the next keys as soon as its fragments of these are in registers.  Two workgroups per compute unit, up to 128 KB of
 // loads on their way.  The waves' outputs are joined through LDS, those of the key range's parts by a second launch.
 constexpr int kTokenTile = 32, kTokenWaves = 4;
+constexpr int kTokenStages = 65536, kTokenLds = kTokenStages + kTokenWaves * kApartBytes;      // bytes of LDS
 
 template <bool E4M3>
 __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAttnArgs a) {
@@ -315,7 +304,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
     constexpr int KT = kTokenTile, NW = kTokenWaves;
     constexpr int kStages = E4M3 ? 2 : 1;
     constexpr int kTile = KT * R::kRow, kLoads = KT / R::kPerLoad;          // bytes and wave loads of a K or V tile
-    static_assert(NW * kStages * 2 * kTile == 65536, "the launch's LDS, which the waves' outputs fill too");
+    static_assert(NW * kStages * 2 * kTile == kTokenStages, "and the waves' outputs fill it too");
     extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
     unsigned char* const k_first = smem;
     unsigned char* const v_first = smem + NW * kTile;
@@ -423,10 +412,12 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
                     for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
             }
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            bf16x8 pf[2];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s0[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[r], a.mask.scale_log2e, -m));
-                sum[r & 3] += s0[r];
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[r], a.mask.scale_log2e, -m));
+                sum[r & 3] += p;
+                pf[r >> 3][r & 7] = (bf16)p;
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             // and these values: behind them went out kStages - 1 tiles and the keys just asked for
@@ -435,18 +426,16 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
             hold_order();
             const unsigned broken = masked ? broken_keys<E4M3>(vt, 0, lane) : 0u;
             if (__builtin_expect(broken != 0, 0)) {
-                add_values_apart<E4M3>(o, vt, 0, s0, broken, lane);
-            } else {
-#pragma unroll
-                for (int ts = 0; ts < 2; ++ts) {
-                    bf16x8 pf;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) pf[e] = (bf16)s0[8 * ts + e];
-#pragma unroll
-                    for (int db = 0; db < 4; ++db)
-                        o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(R::v_fragment(vt + 16 * ts * R::kRow, R::v_lane(lane, db)), pf, o[db], 0, 0, 0);
-                }
+                add_apart<E4M3>(o, vt, 0, pf[0], pf[1], broken, smem + kTokenStages + wave * kApartBytes, lane);
+                if ((broken >> l31) & 1)
+                    for (int c = 0; c < R::kRow / 32; ++c) *reinterpret_cast<uint4*>(vt + l31 * R::kRow + lh * (R::kRow / 2) + c * 16) = uint4{0, 0, 0, 0};
+                reads_done();
             }
+#pragma unroll
+            for (int ts = 0; ts < 2; ++ts)
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(R::v_fragment(vt + 16 * ts * R::kRow, R::v_lane(lane, db)), pf[ts], o[db], 0, 0, 0);
             if (i + kStages < n) {
                 reads_done();
                 fetch(a.v_pages, i + kStages, vt, true);
@@ -559,14 +548,371 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs
     *reinterpret_cast<bf16x8*>(a.o + t * a.o_stride + h * D + c * 8) = out;
 }
 
+// ---------------------------------------------------------------------------------------------------
+// Many rows: NW waves of 32 rows share tiles of 64 keys; the matrix cores bound it, with the vector unit's softmax close behind.
+//   * Scores are computed transposed, S^T = K Q^T: a lane owns a row (column of S^T) with its partner lane + 32, keeps the row's sum and
+//     reference point, and the accumulators are in the order that the second product O^T = V^T P^T takes its P in.
+//   * Keys and values have two stages each.  While the vector unit forms p of tile n, the matrix unit forms S^T of tile n + 1; then
+//     come the values of tile n.  The loads of keys n + 2 and values n + 1 go out between the first products.
+//   * The reference point of a row's exponents trails its maximum by up to kSumLimit's logarithm: a steady tile forms no maximum and
+//     rescales nothing.
+//   * 8-bit pages pass through registers on their way to LDS and are widened there, once per tile: every wave reads every
+//     fragment, and widening those would be eight times the conversions.  They are fetched one tile earlier.
+template <int NW>
+constexpr int kRowsStages = 65536 + (NW == 8 ? 8 * 8192 : 0);
+template <int NW>
+constexpr int kRowsLds = kRowsStages<NW> + NW * kApartBytes + 64;      // bytes of LDS
+
+template <bool E4M3, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows_kernel(PagedAttnArgs a) {
+    typedef Rows<false> R;                                    // in LDS keys and values are bf16 whatever the pages hold
+    constexpr int KT = 64, kTile = KT * 256;
+    constexpr int kRow = E4M3 ? 128 : 256;                    // bytes in a page
+    constexpr int kLoads = KT * kRow / 1024 / NW;             // wave loads of a K or V tile by each wave
+    constexpr int kLoadRows = 1024 / kRow;
+    constexpr int kAhead = E4M3 ? 3 : 2;                      // tiles between the fetch of keys and their softmax
+    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    unsigned char* const k_stage = smem;                      // [2][64 keys][256 B]
+    unsigned char* const v_stage = smem + 2 * kTile;          // [2][64 keys][256 B]
+    constexpr int kStages = kRowsStages<NW>;                  // behind them eight waves' rows, then add_apart's scratch and a word per wave
+    unsigned* const flags = reinterpret_cast<unsigned*>(smem + kStages + NW * kApartBytes);
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l31 = lane & 31, lh = lane >> 5;
+    // Workgroups are handed to the eight XCDs in turn; renumbered, each XCD (its own L2) works through a run of row tiles of the same keys.
+    const unsigned flat = blockIdx.x, xcd = flat & 7u, per = a.n_wg >> 3, rem = a.n_wg & 7u;
+    Work w;
+    if (!locate(a, 32 * NW, xcd * per + min(xcd, rem) + (flat >> 3), &w)) return;
+    const int last_row = min(w.row0 + 32 * NW, w.rows) - 1;
+    const int first_token = (int)divide(w.row0, a.by_group), last_token = (int)divide(last_row, a.by_group);
+    const Visited vis = visited_tiles<KT>(a.mask, w, first_token, last_token);
+    const int first = min(vis.count, w.part * a.part_tiles), end = w.part == a.parts - 1 ? vis.count : min(vis.count, first + a.part_tiles);
+    if (w.part > 0 && first >= end) return;                   // nobody reads this part
+
+    // this lane's row, formed anew where it is needed: kept across the loop it would be spilled
+    auto own_row = [&]() {
+        int t = threadIdx.x;
+        asm volatile("" : "+v"(t));
+        return w.row0 + 32 * (t >> 6) + (t & 31);
+    };
+    struct Place {
+        int token, head;
+        bool live;
+    };
+    auto place_of = [&](int row) {
+        const int r = min(row, w.rows - 1), token = (int)divide(r, a.by_group);
+        return Place{token, w.hk * a.group + r - token * a.group, row < w.rows};
+    };
+
+    f32x16 o[4];
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[db][r] = 0.0f;
+    float m = kNoKey, l = 0.0f;
+
+    if (first < end) {
+        // ---- pages.  Lane g of four looks up the page of sixteen keys of a tile; all four go to every wave, a tile before its keys are
+        // fetched.
+        const int* const table = a.batch.table + (long long)w.seq * a.batch.table_stride;
+        const int slot_mask = (1 << a.batch.page_shift) - 1;
+        auto key_of = [&](int n) { return tile_of(vis, min(n, end - 1)) * KT; };
+        auto look_up = [&](int n) { return table[min((key_of(n) + 16 * (lane & 3)) >> a.batch.page_shift, a.batch.table_stride - 1)]; };
+        struct Source {
+            long long at[kLoads];                             // byte in the pools of this wave's loads of a tile
+        };
+        unsigned gaps_ahead = 0;                              // four bits a tile: sixteen keys without a page
+        auto source_of = [&](int pages, int n, int tiles_ahead) {
+            const bool gone = (unsigned)pages >= (unsigned)a.batch.n_pages;
+            gaps_ahead |= ((unsigned)__builtin_amdgcn_ballot_w64(gone) & 15u) << (4 * tiles_ahead);
+            if (gone) pages = 0;                              // fetched, not seen
+            Source s;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int row = kLoadRows * (wave + NW * i);
+                const long long page = __builtin_amdgcn_readlane(pages, row >> 4);
+                s.at[i] = (((page * a.batch.kv_heads + w.hk) << a.batch.page_shift) + ((key_of(n) + row) & slot_mask)) * kRow;
+            }
+            return s;
+        };
+        // bf16: straight to LDS
+        const int k_lane = (lane >> 4) * 256 + (((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) << 4);
+        const int v_lane = R::v_source(lane, 0);
+        auto fetch = [&](const void* pool, const Source& s, int lane_at, unsigned char* stage) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+                load_to_lds(static_cast<const unsigned char*>(pool) + s.at[i] + lane_at, stage + 1024 * (wave + NW * i));
+        };
+        // e4m3: to registers, and from there as bf16
+        struct Bytes {
+            uint4 x[kLoads];
+        };
+        auto take = [&](const void* pool, const Source& s) {
+            Bytes b;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) b.x[i] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(pool) + s.at[i] + lane * 16);
+            return b;
+        };
+        auto put = [&](const Bytes& b, bool values, unsigned char* stage) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                const int row = 8 * (wave + NW * i) + (lane >> 3), c = 2 * (lane & 7), turn = values ? (row & 3) << 2 : row & 15;
+                *reinterpret_cast<bf16x8*>(stage + row * 256 + ((c ^ turn) << 4)) = widen_e4m3(u32x2{b.x[i].x, b.x[i].y});
+                *reinterpret_cast<bf16x8*>(stage + row * 256 + (((c + 1) ^ turn) << 4)) = widen_e4m3(u32x2{b.x[i].z, b.x[i].w});
+            }
+        };
+
+        // ---- the wave's 32 rows, through LDS: eight waves behind the stages; four in the second stages, which are free until then
+        unsigned char* const q_stage = NW == 8 ? smem + 4 * kTile + wave * 8192 : (wave < 2 ? k_stage : v_stage) + kTile + (wave & 1) * 8192;
+        int pages[kAhead + 1];
+#pragma unroll
+        for (int i = 0; i <= kAhead; ++i) pages[i] = look_up(first + i);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = 4 * i + (lane >> 4);
+            const Place x = place_of(w.row0 + 32 * wave + r);
+            const bf16* src = a.q + (long long)(w.q0 + x.token) * a.q_stride + x.head * D;
+            load_to_lds(reinterpret_cast<const unsigned char*>(src) + (((lane & 15) ^ (r & 15)) << 4), q_stage + i * 1024);
+        }
+        hold_order();
+        Source src0 = source_of(pages[0], first, 0), src1 = source_of(pages[1], first + 1, 1);
+        Source ahead;                                         // of the tile whose values are fetched next
+        Bytes k_bytes, v_bytes, k_one;
+        int next_pages;
+        auto barrier = [&]() {
+            hold_order();
+            __builtin_amdgcn_s_barrier();
+            hold_order();
+        };
+        if constexpr (E4M3) {
+            const Source src2 = source_of(pages[2], first + 2, 2);
+            k_bytes = take(a.k_pages, src0);
+            v_bytes = take(a.v_pages, src0);
+            k_one = take(a.k_pages, src1);
+            const Bytes k_two = take(a.k_pages, src2), v_one = take(a.v_pages, src1);
+            put(k_bytes, false, k_stage);
+            put(v_bytes, true, v_stage);
+            if (NW == 8) put(k_one, false, k_stage + kTile);
+            k_bytes = k_two;
+            v_bytes = v_one;
+            ahead = src2;
+            next_pages = pages[3];
+            __builtin_amdgcn_s_waitcnt(0x0070);               // all loads, and what was put
+        } else {
+            fetch(a.k_pages, src0, k_lane, k_stage);
+            hold_order();
+            fetch(a.v_pages, src0, v_lane, v_stage);
+            hold_order();
+            if (NW == 8) fetch(a.k_pages, src1, k_lane, k_stage + kTile);
+            hold_order();
+            ahead = src1;
+            next_pages = pages[2];
+            __builtin_amdgcn_s_waitcnt(0x0F70 | ((NW == 8 ? 2 : 1) * kLoads));      // the rows and the first keys
+        }
+        barrier();
+        bf16x8 qf[8];
+#pragma unroll
+        for (int s = 0; s < 8; ++s) qf[s] = *reinterpret_cast<const bf16x8*>(q_stage + l31 * 256 + (((2 * s + lh) ^ (l31 & 15)) << 4));
+        if (NW == 4) {
+            reads_done();
+            barrier();                                        // everyone has its rows: the second stages are free
+            if constexpr (E4M3) put(k_one, false, k_stage + kTile);
+            else fetch(a.k_pages, src1, k_lane, k_stage + kTile);
+        }
+
+        // Half of S^T of the tile at sk: steps 4 half .. + 3 of both 32-key blocks, the fragments first, the products in turn to the two
+        // accumulators (one that waits for its own predecessor takes 12 clocks longer).
+        auto qk_half = [&](f32x16 (&s)[2], const unsigned char* sk, int half, auto&& after_reads) {
+            if (half == 0) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[kb][r] = 0.0f;
+            }
+            bf16x8 kf[4][2];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+                    kf[i][kb] = *reinterpret_cast<const bf16x8*>(sk + (kb * 32 + l31) * 256 + (((2 * (4 * half + i) + lh) ^ (l31 & 15)) << 4));
+            after_reads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i][kb], qf[4 * half + i], s[kb], 0, 0, 0);
+        };
+        auto nothing = []() {};
+        int v_at[4];
+#pragma unroll
+        for (int db = 0; db < 4; ++db) v_at[db] = R::v_lane(lane, db);
+
+        const float scale = a.mask.scale_log2e;
+        f32x16 s_a[2], s_b[2];
+        qk_half(s_a, k_stage, 0, nothing);
+        qk_half(s_a, k_stage, 1, nothing);
+
+        // One tile: s_cur holds S^T of tile n; S^T of tile n + 1 is formed into s_nxt on the way.  k_now: keys n + 1; k_fill: keys n + 2 go there;
+        // v_now: values n; v_fill: values n + 1 go there (restrict: a transposing read is taken to wait for every load on its way to LDS
+        // that may alias it).  Past the last tile it is fetched again, unconditionally, into a stage that nobody reads.
+        auto tile_step = [&](const unsigned char* __restrict__ k_now, unsigned char* __restrict__ k_fill, unsigned char* __restrict__ v_now,
+                             unsigned char* __restrict__ v_fill, f32x16 (&s_cur)[2], f32x16 (&s_nxt)[2], int n) __attribute__((always_inline)) {
+            if constexpr (E4M3) __builtin_amdgcn_s_waitcnt(0x0070);
+            else __builtin_amdgcn_s_waitcnt(0x0F70);
+            barrier();                       // keys n + 1 and values n are there; everyone is done with keys n and values n - 1
+            const unsigned gaps = gaps_ahead & 15u;
+            gaps_ahead >>= 4;
+            const int key0 = key_of(n);
+            const bool masked = gaps != 0 || !whole(vis, key0, key0 + KT);
+            if (masked) {
+                // a share of the values each: infinities and NaN need care where a row does not see them (below)
+                bool hit = false;
+#pragma unroll
+                for (int i = 0; i < 16 / NW; ++i) hit |= R::broken(*reinterpret_cast<const uint4*>(v_now + (wave * (16 / NW) + i) * 1024 + lane * 16));
+                const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit);
+                if (lane == 0) flags[wave] = hits != 0;
+                const RowKeys keys = row_keys(a.mask, place_of(own_row()).token, w.n, w.kv_len);
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int j = kb * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
+                        if (!sees(keys, key0 + j) | (((gaps >> (2 * kb + (r >> 3))) & 1) != 0)) s_cur[kb][r] = -INFINITY;
+                    }
+            }
+            const Source src = source_of(next_pages, n + kAhead, kAhead - 1);
+            float sums[4];
+            bf16x8 pf[4];
+            auto exps = [&](int kb) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s_cur[kb][r], scale, -m));
+                    sums[r & 3] = (kb == 0 && r < 4) ? p : sums[r & 3] + p;     // four independent chains
+                    pf[kb * 2 + (r >> 3)][r & 7] = (bf16)p;
+                }
+            };
+            auto pin = [&]() {               // the fragments are formed here, among the products, not after the branch
+#pragma unroll
+                for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(pf[i]));
+            };
+            if constexpr (E4M3) {
+                put(k_bytes, false, k_fill);
+                put(v_bytes, true, v_fill);
+                k_bytes = take(a.k_pages, src);
+                v_bytes = take(a.v_pages, ahead);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            qk_half(s_nxt, k_now, 0, [&]() {
+                if constexpr (!E4M3) {
+                    fetch(a.k_pages, src, k_lane, k_fill);
+                    fetch(a.v_pages, ahead, v_lane, v_fill);
+                }
+            });
+            exps(0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);       // the eight fragment reads, then product | load | vector work
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                if (!E4M3 && i < 2 * kLoads) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            ahead = src;
+            next_pages = look_up(n + kAhead + 1);
+            qk_half(s_nxt, k_now, 1, nothing);
+            exps(1);
+            float lsum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+            pin();
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+                __builtin_amdgcn_sched_group_barrier(0x400, 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(lsum <= kSumLimit)) != 0, 0)) {
+                // a row's scores have run ahead of its reference point (or it has seen no key yet): move it to their maximum
+                const float top = max2(block_max(s_cur[0]), block_max(s_cur[1])) * scale;
+                const bool moved = top > m + kSlack;
+                const float alpha = moved ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
+                m = moved ? top : m;
+                l *= alpha;
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
+                exps(0);
+                exps(1);
+                lsum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                pin();
+            }
+            l += lsum;
+            __builtin_amdgcn_sched_barrier(0);
+            if (masked) {
+                reads_done();
+                barrier();                   // what every wave saw of these values is written down
+                unsigned any = 0;
+#pragma unroll
+                for (int i = 0; i < NW; ++i) any |= flags[i];
+                if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) != 0, 0)) {
+                    const unsigned broken0 = broken_keys<false>(v_now, 0, lane), broken1 = broken_keys<false>(v_now, 32, lane);
+                    unsigned char* const scratch = smem + kStages + wave * kApartBytes;
+                    add_apart<false>(o, v_now, 0, pf[0], pf[1], broken0, scratch, lane);
+                    add_apart<false>(o, v_now, 32, pf[2], pf[3], broken1, scratch, lane);
+                    reads_done();
+                    barrier();               // nobody needs them any more
+                    const unsigned long long all = broken0 | ((unsigned long long)broken1 << 32);
+                    for (int i = threadIdx.x; i < KT * 16; i += 64 * NW)
+                        if ((all >> (i >> 4)) & 1) *reinterpret_cast<uint4*>(v_now + i * 16) = uint4{0, 0, 0, 0};
+                    reads_done();
+                    barrier();
+                }
+            }
+#pragma unroll
+            for (int ts = 0; ts < 4; ++ts)
+#pragma unroll
+                for (int db = 0; db < 4; ++db)
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(R::v_fragment(v_now + 16 * ts * 256, v_at[db]), pf[ts], o[db], 0, 0, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);       // fragment reads (two each) run four ahead of the products
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        for (int n = first; n < end; n += 2) {
+            tile_step(k_stage + kTile, k_stage, v_stage, v_stage + kTile, s_a, s_b, n);
+            if (n + 1 < end) tile_step(k_stage, k_stage + kTile, v_stage + kTile, v_stage, s_b, s_a, n + 1);
+        }
+        __builtin_amdgcn_s_waitcnt(0x0070);      // no load may still be on its way to this LDS when the wave ends
+    }
+    const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    const float total = __uint_as_float(both[0]) + __uint_as_float(both[1]);
+    const Place x = place_of(own_row());
+    store_rows<4>(a, w, x.live, x.token, x.head, m, total, 0, lh == 0, lh, [&](int db, int g, int e) { return o[db][4 * g + e]; });
+}
+
 }  // namespace
 
+// Overrides for tuning runs and tests (sdv2_tuning_set); 0 = the plan's own choice.
+static int g_force_rows = 0, g_force_parts = 0;
+void set_paged_overrides(int rows, int parts) {
+    if (rows >= 0) g_force_rows = rows;
+    if (parts >= 0) g_force_parts = parts;
+}
+
 PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_len, int max_kv_len, int e4m3) {
-    PagedAttnPlan p{32, 1, 1};
     const int group = q_heads / b.kv_heads;
-    const long long wgs = ((long long)b.n_tokens * group / 32 + b.n_seqs) * b.kv_heads;
-    const int tiles = (max_kv_len + 31) / 32;
-    int parts = (int)min((long long)(tiles + 15) / 16, (1024 + wgs - 1) / wgs);
+    const long long rows = (long long)max_q_len * group;
+    PagedAttnPlan p{rows <= 32 ? 32 : rows <= 128 ? 128 : 256, 1, 1};
+    if (g_force_rows > 0) p.rows = g_force_rows;
+    const int key_tile = p.rows == 32 ? 32 : 64;
+    const long long wgs = ((long long)b.n_tokens * group / p.rows + b.n_seqs) * b.kv_heads;
+    const int tiles = (max_kv_len + key_tile - 1) / key_tile;
+    int parts = p.rows == 32 ? (int)min((long long)(tiles + 15) / 16, (1024 + wgs - 1) / wgs) : (int)min((long long)(tiles + 7) / 8, 256 / wgs);
+    if (g_force_parts > 0) parts = min(g_force_parts, tiles);
     if (parts < 1) parts = 1;
     p.part_tiles = max(1, (tiles + parts - 1) / parts);
     p.parts = max(1, (tiles + p.part_tiles - 1) / p.part_tiles);
@@ -574,6 +920,17 @@ PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_l
 }
 
 hipError_t launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan, int e4m3, hipStream_t s) {
+    typedef void (*Kernel)(PagedAttnArgs);
+    static std::once_flag attr_once;
+    static hipError_t attr_err = hipSuccess;
+    std::call_once(attr_once, [&]() {
+        const std::pair<Kernel, int> kernels[] = {{paged_attention_tokens_kernel<false>, kTokenLds}, {paged_attention_tokens_kernel<true>, kTokenLds},
+                                                  {paged_attention_rows_kernel<false, 4>, kRowsLds<4>}, {paged_attention_rows_kernel<true, 4>, kRowsLds<4>},
+                                                  {paged_attention_rows_kernel<false, 8>, kRowsLds<8>}, {paged_attention_rows_kernel<true, 8>, kRowsLds<8>}};
+        for (const auto& k : kernels)
+            if (attr_err == hipSuccess) attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(k.first), hipFuncAttributeMaxDynamicSharedMemorySize, k.second);
+    });
+    if (attr_err != hipSuccess) return attr_err;
     PagedAttnArgs a = args;
     a.parts = plan.parts;
     a.part_tiles = plan.part_tiles;
@@ -583,8 +940,10 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan
     a.by_tiles = fast_div((unsigned)a.row_tiles, (unsigned long long)n_wg);
     a.by_heads = fast_div((unsigned)a.batch.kv_heads, (unsigned long long)n_wg);
     a.by_group = fast_div((unsigned)a.group, (unsigned long long)a.batch.n_tokens * a.group);
-    if (e4m3) hipLaunchKernelGGL(paged_attention_tokens_kernel<true>, dim3(a.n_wg), dim3(256), 65536, s, a);
-    else hipLaunchKernelGGL(paged_attention_tokens_kernel<false>, dim3(a.n_wg), dim3(256), 65536, s, a);
+    auto go = [&](Kernel k, int threads, int lds) { hipLaunchKernelGGL(k, dim3(a.n_wg), dim3(threads), lds, s, a); };
+    if (plan.rows == 32) go(e4m3 ? paged_attention_tokens_kernel<true> : paged_attention_tokens_kernel<false>, 256, kTokenLds);
+    else if (plan.rows == 128) go(e4m3 ? paged_attention_rows_kernel<true, 4> : paged_attention_rows_kernel<false, 4>, 256, kRowsLds<4>);
+    else go(e4m3 ? paged_attention_rows_kernel<true, 8> : paged_attention_rows_kernel<false, 8>, 512, kRowsLds<8>);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && plan.parts > 1) {
         const long long row_heads = (long long)a.batch.n_tokens * a.q_heads;

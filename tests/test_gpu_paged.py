@@ -303,6 +303,39 @@ def test_attention(shape, block, window, sink, e4m3):
     check_attention(c, randn(20 + shape, c.T, q_heads * D), q_heads, block, window, sink)
 
 
+@pytest.fixture
+def form(request):
+    """Rows of a workgroup and parts of the key range, forced for one test."""
+    rows, parts = request.param
+    b.tuning_set("paged_rows", rows)
+    b.tuning_set("paged_parts", parts)
+    yield request.param
+    b.tuning_set("paged_rows", None)
+    b.tuning_set("paged_parts", None)
+
+
+FORMS = [(32, 1), (32, 7), (128, 1), (128, 4), (256, 1), (256, 3)]
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("block,window,sink", [(1, 0, 0), (24, 0, 0), (1, 100, 30)])
+@pytest.mark.parametrize("shape", [2, 4, 5, 6, 7, 8, 9])
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_every_form_of_attention(form, shape, block, window, sink, e4m3):
+    test_attention(shape, block, window, sink, e4m3)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_every_form_keeps_what_is_not_seen_out(form, e4m3):
+    test_what_a_row_does_not_see_does_not_reach_it(130, 500, e4m3, float("nan"))
+    test_attention_does_not_see_pages_that_are_gone(150, e4m3)
+    test_attention_of_strided_rows_and_another_scale(40, e4m3)
+    if not e4m3:
+        test_what_a_row_does_not_see_does_not_reach_it(70, 300, e4m3, float("inf"))
+        test_attention_with_large_scores()
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("q_len", [1, 40, 300])
 def test_attention_of_strided_rows_and_another_scale(q_len, e4m3):

@@ -197,3 +197,10 @@ def test_the_binding_refuses_tensors_that_do_not_fit():
         b.qk_norm_rope(b.rope_cfg(0), None, x, torch.empty_like(x))                      # not on a device
     with pytest.raises(AssertionError):
         b.ragged_batch(torch.zeros(3, dtype=torch.int32), torch.zeros(3, dtype=torch.int32), torch.zeros(3, 2, dtype=torch.int32), 4, 1, 1)
+
+
+@pytest.mark.parametrize("name,value", [("paged_rows", "64"), ("paged_rows", "-32"), ("paged_parts", "-1"), ("paged_parts", "65"), ("paged_parts", "many")])
+def test_tuning_refusals(lib, name, value):
+    with pytest.raises(b.Sdv2Error) as e:
+        b.tuning_set(name, value)
+    assert e.value.code == INVALID
