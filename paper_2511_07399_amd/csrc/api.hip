@@ -2298,18 +2298,19 @@ static const char* lora_wrong(const sdv2_lora_cfg* c) {
     if (c->rank <= 0 || c->rank % 8 || c->rank > 128) return "rank must be a multiple of 8 up to 128";
     if (c->n_adapters <= 0) return "n_adapters must be positive";
     if (c->out_fp32 != 0 && c->out_fp32 != 1) return "out_fp32 must be 0 or 1";
-    if (c->n_seqs <= 0 || c->n_seqs > (1 << 22) || c->n_tokens < 0 || c->n_tokens > (1 << 22) || c->max_q_len < 0) return "n_seqs, n_tokens or max_q_len out of range";
+    if (c->n_seqs <= 0 || c->n_seqs > (1 << 18) || c->n_tokens < 0 || c->n_tokens > (1 << 22) || c->max_q_len < 0) return "n_seqs, n_tokens or max_q_len out of range";
+    if (((int64_t)c->n_tokens / 16 + c->n_seqs) * (c->N / 64) > ((int64_t)1 << 24)) return "too many rows and columns for one call";
     return nullptr;
 }
 
-static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)parts * c->n_tokens * c->rank * sizeof(float), 256); }
+static size_t lora_bytes(const sdv2_lora_cfg* c) { return align_up((size_t)c->n_tokens * 2 * align_up(c->rank, 32) * sizeof(bf16), 256); }
 
 size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg) {
     if (const char* why = lora_wrong(cfg)) {
         fail(SDV2_INVALID_ARG, "%s", why);
         return 0;
     }
-    return lora_bytes(cfg, lora_parts(cfg->n_seqs, cfg->n_tokens, cfg->max_q_len, cfg->K, cfg->rank));
+    return lora_bytes(cfg);
 }
 
 int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* b_dev, const float* scale_dev, const int32_t* adapter_dev,
@@ -2324,8 +2325,7 @@ int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* 
     if (const char* why = rows_wrong(y_dev, y_stride, cfg->N, size)) return fail(SDV2_INVALID_ARG, "y: %s", why);
     if (const char* why = rows_wrong(out_dev, out_stride, cfg->N, size)) return fail(SDV2_INVALID_ARG, "out: %s", why);
     if (out_dev == y_dev && out_stride != y_stride) return fail(SDV2_INVALID_ARG, "in place needs the same stride");
-    const int parts = lora_parts(cfg->n_seqs, cfg->n_tokens, cfg->max_q_len, cfg->K, cfg->rank);
-    const size_t need = lora_bytes(cfg, parts);
+    const size_t need = lora_bytes(cfg);
     if (!workspace_dev || workspace_bytes < need) return fail(SDV2_WORKSPACE_TOO_SMALL, "lora workspace %zu < %zu", workspace_bytes, need);
     if (!aligned16(workspace_dev)) return fail(SDV2_INVALID_ARG, "workspace is not 16-byte aligned");
     LoraArgs a{};
@@ -2347,9 +2347,9 @@ int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* 
     a.rank = cfg->rank;
     a.n_adapters = cfg->n_adapters;
     a.fp32 = cfg->out_fp32;
-    a.u = static_cast<float*>(workspace_dev);
-    a.parts = parts;
-    HIP_TRY(launch_lora(a, static_cast<hipStream_t>(hip_stream)), "adapter kernels");
+    a.u = static_cast<bf16*>(workspace_dev);
+    a.u_ranks = (int)align_up(cfg->rank, 32);
+    HIP_TRY(launch_lora(a, cfg->max_q_len, static_cast<hipStream_t>(hip_stream)), "adapter kernels");
     return SDV2_OK;
 }
 

@@ -126,10 +126,9 @@ struct LoraArgs {
     void* out;
     long long x_stride, y_stride, out_stride;
     int n_seqs, n_tokens, K, N, rank, n_adapters, fp32;
-    float* u;                         // [parts][n_tokens][rank]
-    int parts;
+    bf16* u;                          // scale x A^T: [n_tokens][high, low][u_ranks]
+    int u_ranks;                      // rank rounded up to 32
 };
-int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank);
-hipError_t launch_lora(const LoraArgs& a, hipStream_t s);
+hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s);
 
 }  // namespace sdv2
