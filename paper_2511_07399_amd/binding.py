@@ -772,38 +772,45 @@ def stream_batch_latents_step(h, cfg, mw, io, cache, z_in, frame_pos0, sigmas, e
 
 # ------------------------------------------------------------------------------------------ ragged batches over a paged cache
 # Rows are 2-D tensors whose rows are contiguous, at any stride (slices of a projection's output serve as they are).  Whatever
-# lies on the device has to be on the current one: launches go to its current stream.
-_PAGE_DTYPE = {0: torch.bfloat16, 1: torch.float8_e4m3fn}
+# lies on the device has to be on the current one: launches go to its current stream.  The checks are written for speed: a decode
+# step's calls take the device a few microseconds each, and the first form of these took the host as long.
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+_PAGE_DTYPE = (torch.bfloat16, torch.float8_e4m3fn)
 
 
-def _here(t, dtype):
-    assert t.is_cuda and t.dtype == dtype and t.get_device() == _current_device(), "expected a %s tensor on the current device" % dtype
+def _device_of(t):
+    """Device index of t, which has to be the current device's."""
+    dev = t.get_device()
+    assert dev >= 0 and dev == torch._C._cuda_getDevice(), "expected tensors on the current device"
+    return dev
+
+
+def _dense(t, dtype, dev):
+    assert t.dtype is dtype and t.get_device() == dev and t.is_contiguous(), "expected a contiguous %s tensor on the current device" % dtype
     return t.data_ptr()
 
 
-def _dense(t, dtype):
-    assert t.is_contiguous(), "expected a contiguous tensor"
-    return _here(t, dtype)
-
-
-def _gain(t):
+def _gain(t, dev):
     if t is None:
         return None
     assert t.numel() == HEAD_DIM, "a gain has 128 numbers"
-    return _dense(t, torch.float32)
+    return _dense(t, _F32, dev)
 
 
-def _row_tensor(t, width=None, rows=None, dtype=torch.bfloat16):
-    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), "expected rows of contiguous elements"
-    assert (width is None or t.shape[1] == width) and (rows is None or t.shape[0] == rows), "rows of another shape than expected"
-    # the stride of a tensor of at most one row says nothing, and may be anything
-    return _here(t, dtype), t.stride(0) if t.shape[0] > 1 else max(t.shape[1], 8)
+def _rows(t, dev, width, rows, dtype=_BF16):
+    """(address, stride) of rows of contiguous elements."""
+    n, w = t.shape
+    s0, s1 = t.stride()
+    assert w == width and n == rows and s1 == 1 and t.dtype is dtype and t.get_device() == dev, \
+        "expected %d rows of %d contiguous %s on the current device" % (rows, width, dtype)
+    return t.data_ptr(), s0 if n > 1 else w                  # the stride of a single row says nothing, and may be anything
 
 
-def _heads(t, rows):
-    p, stride = _row_tensor(t, None, rows)
-    assert t.shape[1] % HEAD_DIM == 0, "rows are heads of 128"
-    return p, stride, t.shape[1] // HEAD_DIM
+def _heads(t, dev, rows):
+    width = t.shape[1]
+    assert width % HEAD_DIM == 0 and width > 0, "rows are heads of 128"
+    p, stride = _rows(t, dev, width, rows)
+    return p, stride, width // HEAD_DIM
 
 
 def rope_cfg(axes, halves=False, base=10000.0, eps=1e-6):
@@ -827,11 +834,12 @@ def paged_pool_bytes(cfg):
 def ragged_batch(q_start, kv_len, page_table, n_tokens, max_q_len, max_kv_len):
     """q_start: device int32 [n_seqs + 1]; kv_len: device int32 [n_seqs], after the append; page_table: device int32
     [n_seqs, entries].  The struct keeps the three tensors alive."""
-    n = kv_len.numel()
+    n, dev = kv_len.numel(), _device_of(kv_len)
     assert q_start.numel() == n + 1 and page_table.dim() == 2 and page_table.shape[0] == n, "arrays of different batches"
-    b = RaggedBatch(C.sizeof(RaggedBatch), n, n_tokens, max_q_len, max_kv_len, page_table.shape[1], _dense(q_start, torch.int32),
-                    _dense(kv_len, torch.int32), _dense(page_table, torch.int32))
+    b = RaggedBatch(C.sizeof(RaggedBatch), n, n_tokens, max_q_len, max_kv_len, page_table.shape[1], _dense(q_start, _I32, dev),
+                    _dense(kv_len, _I32, dev), _dense(page_table, _I32, dev))
     b.tensors = (q_start, kv_len, page_table)
+    b.device = dev
     return b
 
 
@@ -840,43 +848,53 @@ def attn_mask(block=0, window=0, sink=0, scale=0.0):
     return AttnMask(C.sizeof(AttnMask), block, window, sink, scale)
 
 
-def _positions(rope, pos, rows):
+def _positions(rope, pos, rows, dev):
     if rope is None or rope.axes == 0:
         return None
     assert pos.numel() == rows * rope.axes, "positions are [rows, axes]"
-    return _dense(pos, torch.int32)
+    return _dense(pos, _I32, dev)
+
+
+_NO_ROWS = (None, 0, 0, None, None, 0)
+
+
+def _turned(t, out, gain, dev, rows):
+    """The six arguments of rows that are normed and turned."""
+    if t is None:
+        return _NO_ROWS
+    p, stride, heads = _heads(t, dev, rows)
+    po, out_stride = _rows(out, dev, heads * HEAD_DIM, rows)
+    return p, stride, heads, _gain(gain, dev), po, out_stride
 
 
 def qk_norm_rope(rope, positions, q, q_out, g_q=None, k=None, k_out=None, g_k=None):
     """q, k (either may be None): bf16 rows of heads; the outputs may be the inputs.  positions: device int32 [rows, axes]."""
     load_library()
-    T = (k if q is None else q).shape[0]
-    qp, qs, qh = (None, 0, 0) if q is None else _heads(q, T)
-    kp, ks, kh = (None, 0, 0) if k is None else _heads(k, T)
-    qo, qos = (None, 0) if q is None else _row_tensor(q_out, q.shape[1], T)
-    ko, kos = (None, 0) if k is None else _row_tensor(k_out, k.shape[1], T)
-    _check(_lib.sdv2_qk_norm_rope(C.addressof(rope), T, _positions(rope, positions, T), qp, qs, qh, _gain(g_q), qo, qos,
-                                  kp, ks, kh, _gain(g_k), ko, kos, _stream()))
+    one = k if q is None else q
+    T, dev = one.shape[0], _device_of(one)
+    rc = _lib.sdv2_qk_norm_rope(C.addressof(rope), T, _positions(rope, positions, T, dev), *_turned(q, q_out, g_q, dev, T),
+                                *_turned(k, k_out, g_k, dev, T), torch._C._cuda_getCurrentRawStream(dev))
+    if rc != OK:
+        _check(rc)
 
 
-def _pages(cfg, k_pages, v_pages):
+def _pages(cfg, k_pages, v_pages, dev):
     shape = (cfg.n_pages, cfg.kv_heads, cfg.page_tokens, HEAD_DIM)
     dtype = _PAGE_DTYPE[cfg.format]
-    assert tuple(k_pages.shape) == shape and tuple(v_pages.shape) == shape, "pools are [n_pages, kv_heads, page_tokens, 128]"
-    return _dense(k_pages, dtype), _dense(v_pages, dtype)
+    assert k_pages.shape == shape and v_pages.shape == shape, "pools are [n_pages, kv_heads, page_tokens, 128]"
+    return _dense(k_pages, dtype, dev), _dense(v_pages, dtype, dev)
 
 
 def paged_append(cfg, k_pages, v_pages, batch, k, v, rope=None, positions=None, g_k=None, q=None, q_out=None, g_q=None):
     """k, v: bf16 rows of the batch's new tokens.  With rope, k (and q, to q_out) get norm (with a gain) and rotation on the way."""
     load_library()
-    T = batch.n_tokens
-    kp, vp = _pages(cfg, k_pages, v_pages)
-    kr, ks = _row_tensor(k, cfg.kv_heads * HEAD_DIM, T)
-    vr, vs = _row_tensor(v, cfg.kv_heads * HEAD_DIM, T)
-    qp, qs, qh = (None, 0, 0) if q is None else _heads(q, T)
-    qo, qos = (None, 0) if q is None else _row_tensor(q_out, q.shape[1], T)
-    _check(_lib.sdv2_paged_append(C.addressof(cfg), kp, vp, C.addressof(batch), None if rope is None else C.addressof(rope),
-                                  _positions(rope, positions, T), kr, ks, _gain(g_k), vr, vs, qp, qs, qh, _gain(g_q), qo, qos, _stream()))
+    T, width, dev = batch.n_tokens, cfg.kv_heads * HEAD_DIM, _device_of(k_pages)
+    assert batch.device == dev, "batch of another device"
+    rc = _lib.sdv2_paged_append(C.addressof(cfg), *_pages(cfg, k_pages, v_pages, dev), C.addressof(batch), None if rope is None else C.addressof(rope),
+                                _positions(rope, positions, T, dev), *_rows(k, dev, width, T), _gain(g_k, dev), *_rows(v, dev, width, T),
+                                *_turned(q, q_out, g_q, dev, T), torch._C._cuda_getCurrentRawStream(dev))
+    if rc != OK:
+        _check(rc)
 
 
 def paged_attention_workspace_bytes(cfg, batch, mask, q_heads):
@@ -884,15 +902,26 @@ def paged_attention_workspace_bytes(cfg, batch, mask, q_heads):
     return _lib.sdv2_paged_attention_workspace_bytes(C.addressof(cfg), C.addressof(batch), C.addressof(mask), q_heads)
 
 
+def _scratch(workspace, dev):
+    if workspace is None:
+        return None, 0
+    assert workspace.get_device() == dev and workspace.is_contiguous(), "expected a workspace on the current device"
+    return workspace.data_ptr(), workspace.nbytes
+
+
 def paged_attention(cfg, k_pages, v_pages, batch, mask, q, o, workspace=None):
     """q, o: bf16 rows [n_tokens, q_heads * 128]."""
     load_library()
-    T = batch.n_tokens
-    kp, vp = _pages(cfg, k_pages, v_pages)
-    qp, qs, qh = _heads(q, T)
-    op, os_ = _row_tensor(o, q.shape[1], T)
-    _check(_lib.sdv2_paged_attention(C.addressof(cfg), kp, vp, C.addressof(batch), C.addressof(mask), qp, qs, qh, op, os_, _ptr(workspace),
-                                     0 if workspace is None else workspace.nbytes, _stream()))
+    T, dev = batch.n_tokens, _device_of(q)
+    assert batch.device == dev, "batch of another device"
+    p, stride, heads = _heads(q, dev, T)
+    rc = _lib.sdv2_paged_attention(C.addressof(cfg), *_pages(cfg, k_pages, v_pages, dev), C.addressof(batch), C.addressof(mask), p, stride, heads,
+                                   *_rows(o, dev, heads * HEAD_DIM, T), *_scratch(workspace, dev), torch._C._cuda_getCurrentRawStream(dev))
+    if rc != OK:
+        _check(rc)
+
+
+_LORA_CFG_BYTES = C.sizeof(LoraCfg)
 
 
 def lora_cfg(K, N, rank, n_adapters, n_seqs, n_tokens, max_q_len, fp32=False):
@@ -909,12 +938,12 @@ def lora_bf16(x, a, b, scale, adapter, q_start, max_q_len, y, out, workspace):
     adapter int32 [n_seqs] (outside [0, n_adapters): none), q_start int32 [n_seqs + 1]; y and out of one type, bf16 or fp32."""
     load_library()
     n, rank, K = a.shape
-    N, T, fp32 = b.shape[1], x.shape[0], y.dtype == torch.float32
-    assert tuple(b.shape) == (n, N, rank) and q_start.numel() == adapter.numel() + 1 and (scale is None or scale.numel() == n), "shapes disagree"
-    xp, xs = _row_tensor(x, K, T)
-    yp, ys = _row_tensor(y, N, T, torch.float32 if fp32 else torch.bfloat16)
-    op, os_ = _row_tensor(out, N, T, y.dtype)
-    cfg = lora_cfg(K, N, rank, n, adapter.numel(), T, max_q_len, fp32)
-    _check(_lib.sdv2_lora_bf16(C.addressof(cfg), _dense(a, torch.bfloat16), _dense(b, torch.bfloat16),
-                               None if scale is None else _dense(scale, torch.float32), _dense(adapter, torch.int32), _dense(q_start, torch.int32),
-                               xp, xs, yp, ys, op, os_, _ptr(workspace), 0 if workspace is None else workspace.nbytes, _stream()))
+    N, T, dev, n_seqs, dtype = b.shape[1], x.shape[0], _device_of(x), adapter.numel(), y.dtype
+    assert b.shape == (n, N, rank) and q_start.numel() == n_seqs + 1 and (scale is None or scale.numel() == n), "shapes disagree"
+    assert dtype is _BF16 or dtype is _F32, "rows are bf16 or fp32"
+    cfg = LoraCfg(_LORA_CFG_BYTES, K, N, rank, n, dtype is _F32, n_seqs, T, max_q_len)
+    rc = _lib.sdv2_lora_bf16(C.addressof(cfg), _dense(a, _BF16, dev), _dense(b, _BF16, dev), None if scale is None else _dense(scale, _F32, dev),
+                             _dense(adapter, _I32, dev), _dense(q_start, _I32, dev), *_rows(x, dev, K, T), *_rows(y, dev, N, T, dtype),
+                             *_rows(out, dev, N, T, dtype), *_scratch(workspace, dev), torch._C._cuda_getCurrentRawStream(dev))
+    if rc != OK:
+        _check(rc)

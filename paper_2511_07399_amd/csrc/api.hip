@@ -2239,6 +2239,16 @@ static const char* paged_attention_wrong(const sdv2_paged_cfg* cfg, const sdv2_r
     return nullptr;
 }
 
+static MaskArgs mask_args(const sdv2_attn_mask* m, const sdv2_paged_cfg* cfg) {
+    MaskArgs a{};
+    a.block = m->block;
+    a.window = m->window;
+    a.sink = m->sink;
+    const float scale = m->scale > 0.0f ? m->scale : 1.0f / sqrtf((float)SDV2_HEAD_DIM);
+    a.scale_log2e = scale * 1.4426950408889634f * cfg->k_scale;
+    return a;
+}
+
 static size_t paged_attention_bytes(const PagedAttnPlan& plan, int64_t row_heads) {
     return plan.parts > 1 ? (size_t)plan.parts * row_heads * (SDV2_HEAD_DIM + 2) * sizeof(float) : 0;
 }
@@ -2248,7 +2258,7 @@ size_t sdv2_paged_attention_workspace_bytes(const sdv2_paged_cfg* cfg, const sdv
         fail(SDV2_INVALID_ARG, "%s", why);
         return 0;
     }
-    const PagedAttnPlan plan = plan_paged_attention(ragged_args(batch, cfg), q_heads, batch->max_q_len, batch->max_kv_len, cfg->format == SDV2_PAGES_E4M3);
+    const PagedAttnPlan plan = plan_paged_attention(ragged_args(batch, cfg), mask_args(mask, cfg), q_heads, batch->max_q_len, batch->max_kv_len, cfg->format == SDV2_PAGES_E4M3);
     return paged_attention_bytes(plan, (int64_t)batch->n_tokens * q_heads);
 }
 
@@ -2264,17 +2274,13 @@ int32_t sdv2_paged_attention(const sdv2_paged_cfg* cfg, const void* k_pages_dev,
     if (const char* why = rows_wrong(o_dev, o_stride, width, 2)) return fail(SDV2_INVALID_ARG, "o: %s", why);
     PagedAttnArgs a{};
     a.batch = ragged_args(batch, cfg);
+    a.mask = mask_args(mask, cfg);
     const int e4m3 = cfg->format == SDV2_PAGES_E4M3;
-    const PagedAttnPlan plan = plan_paged_attention(a.batch, q_heads, batch->max_q_len, batch->max_kv_len, e4m3);
+    const PagedAttnPlan plan = plan_paged_attention(a.batch, a.mask, q_heads, batch->max_q_len, batch->max_kv_len, e4m3);
     const int64_t row_heads = (int64_t)batch->n_tokens * q_heads;
     const size_t need = paged_attention_bytes(plan, row_heads);
     if (need > 0 && (!workspace_dev || workspace_bytes < need)) return fail(SDV2_WORKSPACE_TOO_SMALL, "paged attention workspace %zu < %zu", workspace_bytes, need);
     if (need > 0 && !aligned16(workspace_dev)) return fail(SDV2_INVALID_ARG, "workspace is not 16-byte aligned");
-    a.mask.block = mask->block;
-    a.mask.window = mask->window;
-    a.mask.sink = mask->sink;
-    const float scale = mask->scale > 0.0f ? mask->scale : 1.0f / sqrtf((float)SDV2_HEAD_DIM);
-    a.mask.scale_log2e = scale * 1.4426950408889634f * cfg->k_scale;
     a.q = static_cast<const bf16*>(q_dev);
     a.o = static_cast<bf16*>(o_dev);
     a.q_stride = q_stride;

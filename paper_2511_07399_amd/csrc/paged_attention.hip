@@ -76,12 +76,7 @@ struct Work {
 
 // Row tiles are numbered without a table: those of sequence s start at floor(q_start[s] group / tile) + s, which leaves each sequence
 // at least as many numbers as it has tiles.  False: a number that no tile has.
-__device__ __forceinline__ bool locate(const PagedAttnArgs& a, int tile_rows, unsigned logical, Work* w) {
-    const unsigned rest = divide(logical, a.by_tiles), z = divide(rest, a.by_heads);
-    // the last tiles of a causal prompt see the most keys: they go first
-    const int tile = a.row_tiles - 1 - (int)(logical - rest * a.by_tiles.d);
-    w->hk = (int)(rest - z * a.by_heads.d);
-    w->part = (int)z;
+__device__ __forceinline__ bool locate(const PagedAttnArgs& a, int tile_rows, int tile, Work* w) {
     auto start = [&](int s) { return (int)((long long)a.batch.q_start[s] * a.group / tile_rows) + s; };
     w->seq = find_sequence(a.batch.n_seqs, tile, start);
     if (w->seq >= a.batch.n_seqs) return false;
@@ -290,6 +285,13 @@ __device__ __forceinline__ void store_rows(const PagedAttnArgs& a, const Work& w
     }
 }
 
+// What a part that has no keys leaves for the join.
+__device__ __forceinline__ void no_keys(const PagedAttnArgs& a, const Work& w, int token, int head) {
+    float* const ml = a.part_ml + (((long long)w.part * a.batch.n_tokens + w.q0 + token) * a.q_heads + head) * 2;
+    ml[0] = kNoKey;
+    ml[1] = 0.0f;
+}
+
 // ---------------------------------------------------------------------------------------------------
 // Few rows: the keys are what is read, and the memory what bounds it.  A workgroup has at most 32 rows; its four waves take the key
 // tiles of 32 in turn, each with a buffer of its own in LDS that direct loads fill and no barrier guards: a wave waits for its own loads
@@ -313,17 +315,26 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l31 = lane & 31, lh = lane >> 5;
+    // Workgroups go to the eight XCDs in turn, so the heads of a sequence come one after the other: with the sequences next to each
+    // other, an XCD has every eighth of them where their number allows, and the XCD with the longest is waited for (64 sequences of
+    // 1 to 16 000 keys: 395 us, this order 350).
     Work w;
-    if (!locate(a, KT, blockIdx.x, &w)) return;
+    const unsigned rest = divide(blockIdx.x, a.by_heads), part = divide(rest, a.by_tiles);
+    w.hk = (int)(blockIdx.x - rest * a.by_heads.d);
+    w.part = (int)part;
+    if (!locate(a, KT, (int)(rest - part * a.by_tiles.d), &w)) return;
     const int last_row = min(w.row0 + 32, w.rows) - 1;
     const Visited vis = visited_tiles<KT>(a.mask, w, w.row0 / a.group, last_row / a.group);
     const int first = min(vis.count, w.part * a.part_tiles), end = w.part == a.parts - 1 ? vis.count : min(vis.count, first + a.part_tiles);
-    if (w.part > 0 && first >= end) return;                                  // nobody reads this part
     const int count = max(0, (end - first - wave + NW - 1) / NW);           // tiles of this wave
 
     // this lane's row
     const int row = min(w.row0 + l31, w.rows - 1), token = (int)divide(row, a.by_group), head = w.hk * a.group + row - token * a.group;
     const bool live = w.row0 + l31 < w.rows;
+    if (a.parts > 1 && first >= end) {
+        if (wave == 0 && lh == 0 && live) no_keys(a, w, token, head);
+        return;
+    }
     const RowKeys keys = row_keys(a.mask, token, w.n, w.kv_len);
     bf16x8 qf[8];
     {
@@ -504,47 +515,77 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
     store_rows<1>(a, w, live, token, head, top, total, 32 * wave, wave == 0 && lh == 0, lh, [&](int, int g, int e) { return mine[g][e]; });
 }
 
-// Second launch where the key range is in parts: out = sum_i 2^(m_i - max m) O_i / sum_i 2^(m_i - max m) l_i over the parts that the row's
-// workgroup had.  Sixteen lanes a row and head, eight channels each.
-__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs a, int tile_rows, int key_tile) {
+// Second launch where the key range is in parts: out = sum_i 2^(m_i - max m) O_i / sum_i 2^(m_i - max m) l_i.  A part that saw no key of the
+// row has left l = 0 and no O.  Sixteen lanes have eight channels each of a row and head, and GROUPS such groups take its parts in turn:
+// one group, and the parts of a single token are a chain of loads (36 of them: 10.8 us, sixteen groups 4).
+template <int GROUPS>
+__global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs a) {
+    __shared__ f32x4 sums[GROUPS == 1 ? 1 : 256][2];
+    __shared__ float ml[GROUPS == 1 ? 1 : 256][2];
     const long long row_heads = (long long)a.batch.n_tokens * a.q_heads;
-    const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) >> 4;
-    const int c = threadIdx.x & 15;
-    const int t = (int)(min(at, row_heads - 1) / a.q_heads), h = (int)(min(at, row_heads - 1) - (long long)t * a.q_heads);
-    // the sequence, row by row: lanes of a wave may be of several
-    int lo = 0, hi = a.batch.n_seqs;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (a.batch.q_start[mid + 1] <= t) lo = mid + 1;
-        else hi = mid;
-    }
-    if (at >= row_heads || lo >= a.batch.n_seqs) return;
-    Work w;
-    w.q0 = a.batch.q_start[lo];
-    w.n = a.batch.q_start[lo + 1] - w.q0;
-    w.kv_len = (int)min((long long)a.batch.kv_len[lo], (long long)a.batch.table_stride << a.batch.page_shift);
-    if (w.q0 < 0 || t < w.q0 || w.n > a.batch.n_tokens - w.q0) return;
-    // the workgroup that had this row, and so how many parts its keys were in
-    const int row = (t - w.q0) * a.group + h % a.group, row0 = row / tile_rows * tile_rows, last = min(row0 + tile_rows, w.n * a.group) - 1;
-    const int count = key_tile == 32 ? visited_tiles<32>(a.mask, w, row0 / a.group, last / a.group).count
-                                     : visited_tiles<64>(a.mask, w, row0 / a.group, last / a.group).count;
-    const int parts = min(a.parts, max(1, (count + a.part_tiles - 1) / a.part_tiles));
-    float top = kNoKey;
-    for (int p = 0; p < parts; ++p) top = fmaxf(top, a.part_ml[(p * row_heads + at) * 2]);
-    float acc[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f}, total = 0.0f;
-    for (int p = 0; p < parts; ++p) {
-        const float* ml = a.part_ml + (p * row_heads + at) * 2;
-        const float weight = __builtin_amdgcn_exp2f(ml[0] - top);
-        total += weight * ml[1];
-        const f32x4* op = reinterpret_cast<const f32x4*>(a.part_o + (p * row_heads + at) * D + c * 8);
-        const f32x4 x = op[0], y = op[1];
+    const int group = (threadIdx.x >> 4) % GROUPS, c = threadIdx.x & 15;
+    const long long at = (long long)blockIdx.x * (16 / GROUPS) + threadIdx.x / (16 * GROUPS);
+    const int t = (int)(at / a.q_heads), h = (int)(at - (long long)t * a.q_heads);
+    const bool live = at < row_heads && t < a.batch.q_start[a.batch.n_seqs];        // behind the last sequence nothing is written
+    float top = kNoKey, total = 0.0f;
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f}, y = x;
+    if (live) {
+        constexpr int kAtOnce = 4;
+        for (int p0 = group; p0 < a.parts; p0 += GROUPS * kAtOnce) {
+            float m[kAtOnce], l[kAtOnce];
+            f32x4 u[kAtOnce], v[kAtOnce];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e] += weight * (e < 4 ? x[e & 3] : y[e & 3]);
+            for (int i = 0; i < kAtOnce; ++i) {
+                const int p = p0 + GROUPS * i;
+                const bool in = p < a.parts;
+                const float* const q = a.part_ml + ((in ? p : p0) * row_heads + at) * 2;
+                m[i] = q[0];
+                l[i] = in ? q[1] : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (l[i] == 0.0f) continue;
+                const f32x4* const q = reinterpret_cast<const f32x4*>(a.part_o + ((p0 + GROUPS * i) * row_heads + at) * D + c * 8);
+                u[i] = q[0];
+                v[i] = q[1];
+            }
+#pragma unroll
+            for (int i = 0; i < kAtOnce; ++i) {
+                if (l[i] == 0.0f) continue;
+                const float next = fmaxf(top, m[i]), keep = __builtin_amdgcn_exp2f(top - next), weight = __builtin_amdgcn_exp2f(m[i] - next);
+                top = next;
+                total = total * keep + l[i] * weight;
+                x = x * keep + u[i] * weight;
+                y = y * keep + v[i] * weight;
+            }
+        }
     }
+    if (GROUPS > 1) {
+        sums[threadIdx.x][0] = x;
+        sums[threadIdx.x][1] = y;
+        ml[threadIdx.x][0] = top;
+        ml[threadIdx.x][1] = total;
+        __syncthreads();
+        if (group != 0 || !live) return;
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g) top = fmaxf(top, ml[threadIdx.x + 16 * g][0]);
+        const float own = __builtin_amdgcn_exp2f(ml[threadIdx.x][0] - top);
+        total *= own;
+        x *= own;
+        y *= own;
+#pragma unroll
+        for (int g = 1; g < GROUPS; ++g) {
+            const float weight = __builtin_amdgcn_exp2f(ml[threadIdx.x + 16 * g][0] - top);
+            total += weight * ml[threadIdx.x + 16 * g][1];
+            x += weight * sums[threadIdx.x + 16 * g][0];
+            y += weight * sums[threadIdx.x + 16 * g][1];
+        }
+    }
+    if (!live) return;
     const float inv = total != 0.0f ? a.v_scale / total : 0.0f;
     bf16x8 out;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) out[e] = (bf16)(acc[e] * inv);
+    for (int e = 0; e < 8; ++e) out[e] = (bf16)((e < 4 ? x[e & 3] : y[e & 3]) * inv);
     *reinterpret_cast<bf16x8*>(a.o + t * a.o_stride + h * D + c * 8) = out;
 }
 
@@ -579,16 +620,18 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l31 = lane & 31, lh = lane >> 5;
-    // Workgroups are handed to the eight XCDs in turn; renumbered, each XCD (its own L2) works through a run of row tiles of the same keys.
+    // Workgroups are handed to the eight XCDs in turn; renumbered, each XCD (its own L2) works through a run of row tiles of the same keys,
+    // the last tile first: under a causal mask it sees the most keys.
     const unsigned flat = blockIdx.x, xcd = flat & 7u, per = a.n_wg >> 3, rem = a.n_wg & 7u;
+    const unsigned logical = xcd * per + min(xcd, rem) + (flat >> 3), rest = divide(logical, a.by_tiles), part = divide(rest, a.by_heads);
     Work w;
-    if (!locate(a, 32 * NW, xcd * per + min(xcd, rem) + (flat >> 3), &w)) return;
+    w.hk = (int)(rest - part * a.by_heads.d);
+    w.part = (int)part;
+    if (!locate(a, 32 * NW, a.row_tiles - 1 - (int)(logical - rest * a.by_tiles.d), &w)) return;
     const int last_row = min(w.row0 + 32 * NW, w.rows) - 1;
     const int first_token = (int)divide(w.row0, a.by_group), last_token = (int)divide(last_row, a.by_group);
     const Visited vis = visited_tiles<KT>(a.mask, w, first_token, last_token);
     const int first = min(vis.count, w.part * a.part_tiles), end = w.part == a.parts - 1 ? vis.count : min(vis.count, first + a.part_tiles);
-    if (w.part > 0 && first >= end) return;                   // nobody reads this part
-
     // this lane's row, formed anew where it is needed: kept across the loop it would be spilled
     auto own_row = [&]() {
         int t = threadIdx.x;
@@ -603,6 +646,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
         const int r = min(row, w.rows - 1), token = (int)divide(r, a.by_group);
         return Place{token, w.hk * a.group + r - token * a.group, row < w.rows};
     };
+    if (a.parts > 1 && first >= end) {
+        const Place x = place_of(own_row());
+        if (lh == 0 && x.live) no_keys(a, w, x.token, x.head);
+        return;
+    }
 
     f32x16 o[4];
 #pragma unroll
@@ -903,18 +951,33 @@ void set_paged_overrides(int rows, int parts) {
     if (parts >= 0) g_force_parts = parts;
 }
 
-PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_len, int max_kv_len, int e4m3) {
+// Parts of the key range where workgroups have 32 rows.  Memory serves the compute units alike, so a unit with two workgroups finishes
+// after the units with one; many small parts even that out and even out the lengths, which only the device knows.  A part costs a
+// workgroup's start (4 us) and the join's reading: it is worth 512 keys (8-bit pages, half the bytes: 1024).  With less than a
+// workgroup per unit the chain of a workgroup's tiles is the time, and 128 keys, one tile a wave, are worth a part.  us, bf16, 8 key
+// heads, equal lengths, this rule / best number of parts: 64 x 7584 keys 346 / 335, 32 x 12 000 276 / 270, 32 x 700 24.9 / 23.3, 12 x 3000
+// 38.7 / 35.0, 4 x 3000 17.3 / 17.3, 4 x 700 11.7 / 11.7, 1 x 12 000 17.5 / 17.4, 1 x 3000 12.4 / 12.4.  64 x 1 to 16 000: 367 / 363, one
+// part 387.
+static int token_parts(long long workgroups, int keys, int e4m3) {
+    const long long spread = min((2048 + workgroups - 1) / workgroups, (long long)(keys / (e4m3 ? 1024 : 512)));
+    const long long chain = min(kUnits / workgroups, (long long)(keys / 128));
+    return (int)max(max(spread, chain >= 4 ? chain : 1ll), 1ll);
+}
+
+PagedAttnPlan plan_paged_attention(const RaggedArgs& b, const MaskArgs& mask, int q_heads, int max_q_len, int max_kv_len, int e4m3) {
     const int group = q_heads / b.kv_heads;
     const long long rows = (long long)max_q_len * group;
     PagedAttnPlan p{rows <= 32 ? 32 : rows <= 128 ? 128 : 256, 1, 1};
     if (g_force_rows > 0) p.rows = g_force_rows;
     const int key_tile = p.rows == 32 ? 32 : 64;
-    const long long wgs = ((long long)b.n_tokens * group / p.rows + b.n_seqs) * b.kv_heads;
-    const int tiles = (max_kv_len + key_tile - 1) / key_tile;
-    int parts = p.rows == 32 ? (int)min((long long)(tiles + 15) / 16, (1024 + wgs - 1) / wgs) : (int)min((long long)(tiles + 7) / 8, 256 / wgs);
+    // keys that a workgroup's rows see at most
+    long long keys = max_kv_len;
+    if (mask.window > 0) keys = min(keys, (long long)mask.window + mask.sink + min(max_q_len, p.rows / group + 1) + mask.block);
+    const int tiles = (int)((keys + key_tile - 1) / key_tile);
+    const long long wgs = max((long long)b.n_tokens * group / p.rows, (long long)b.n_seqs) * b.kv_heads;
+    int parts = p.rows == 32 ? token_parts(wgs, (int)keys, e4m3) : (int)min((long long)(tiles + 7) / 8, 256 / wgs);
     if (g_force_parts > 0) parts = min(g_force_parts, tiles);
-    if (parts < 1) parts = 1;
-    p.part_tiles = max(1, (tiles + parts - 1) / parts);
+    p.part_tiles = max(1, (tiles + max(parts, 1) - 1) / max(parts, 1));
     p.parts = max(1, (tiles + p.part_tiles - 1) / p.part_tiles);
     return p;
 }
@@ -947,7 +1010,11 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && plan.parts > 1) {
         const long long row_heads = (long long)a.batch.n_tokens * a.q_heads;
-        hipLaunchKernelGGL(paged_attention_join_kernel, dim3((unsigned)((row_heads + 15) / 16)), dim3(256), 0, s, a, plan.rows, plan.rows == 32 ? 32 : 64);
+        const int groups = plan.parts > 16 && row_heads <= 4096 ? 16 : plan.parts > 4 && row_heads <= 16384 ? 4 : 1;
+        const dim3 grid((unsigned)((row_heads * groups + 15) / 16));
+        if (groups == 16) hipLaunchKernelGGL(paged_attention_join_kernel<16>, grid, dim3(256), 0, s, a);
+        else if (groups == 4) hipLaunchKernelGGL(paged_attention_join_kernel<4>, grid, dim3(256), 0, s, a);
+        else hipLaunchKernelGGL(paged_attention_join_kernel<1>, grid, dim3(256), 0, s, a);
         e = hipGetLastError();
     }
     return e;

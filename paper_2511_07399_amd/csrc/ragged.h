@@ -110,7 +110,7 @@ struct PagedAttnPlan {
     int rows;                         // rows (tokens times group) of a workgroup: 32, keys over its waves; 128 or 256, rows over its waves
     int parts, part_tiles;
 };
-PagedAttnPlan plan_paged_attention(const RaggedArgs& b, int q_heads, int max_q_len, int max_kv_len, int e4m3);
+PagedAttnPlan plan_paged_attention(const RaggedArgs& b, const MaskArgs& mask, int q_heads, int max_q_len, int max_kv_len, int e4m3);
 // Tuning hooks: rows of a workgroup (32, 128, 256) and parts of the key range (0 = planner); -1 leaves a value as is.
 void set_paged_overrides(int rows, int parts);
 hipError_t launch_paged_attention(const PagedAttnArgs& a, const PagedAttnPlan& plan, int e4m3, hipStream_t s);
