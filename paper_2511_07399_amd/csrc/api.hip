@@ -2309,14 +2309,14 @@ static const char* lora_wrong(const sdv2_lora_cfg* c) {
     return nullptr;
 }
 
-static size_t lora_bytes(const sdv2_lora_cfg* c) { return align_up((size_t)c->n_tokens * 2 * align_up(c->rank, 32) * sizeof(bf16), 256); }
+static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)parts * c->n_tokens * align_up(c->rank, 16) * sizeof(float), 256); }
 
 size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg) {
     if (const char* why = lora_wrong(cfg)) {
         fail(SDV2_INVALID_ARG, "%s", why);
         return 0;
     }
-    return lora_bytes(cfg);
+    return lora_bytes(cfg, lora_parts(cfg->n_seqs, cfg->n_tokens, cfg->max_q_len, cfg->K, cfg->rank));
 }
 
 int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* b_dev, const float* scale_dev, const int32_t* adapter_dev,
@@ -2331,7 +2331,8 @@ int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* 
     if (const char* why = rows_wrong(y_dev, y_stride, cfg->N, size)) return fail(SDV2_INVALID_ARG, "y: %s", why);
     if (const char* why = rows_wrong(out_dev, out_stride, cfg->N, size)) return fail(SDV2_INVALID_ARG, "out: %s", why);
     if (out_dev == y_dev && out_stride != y_stride) return fail(SDV2_INVALID_ARG, "in place needs the same stride");
-    const size_t need = lora_bytes(cfg);
+    const int parts = lora_parts(cfg->n_seqs, cfg->n_tokens, cfg->max_q_len, cfg->K, cfg->rank);
+    const size_t need = lora_bytes(cfg, parts);
     if (!workspace_dev || workspace_bytes < need) return fail(SDV2_WORKSPACE_TOO_SMALL, "lora workspace %zu < %zu", workspace_bytes, need);
     if (!aligned16(workspace_dev)) return fail(SDV2_INVALID_ARG, "workspace is not 16-byte aligned");
     LoraArgs a{};
@@ -2353,8 +2354,9 @@ int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* 
     a.rank = cfg->rank;
     a.n_adapters = cfg->n_adapters;
     a.fp32 = cfg->out_fp32;
-    a.u = static_cast<bf16*>(workspace_dev);
-    a.u_ranks = (int)align_up(cfg->rank, 32);
+    a.u = workspace_dev;
+    a.u_ranks = (int)align_up(cfg->rank, 16);
+    a.parts = parts;
     HIP_TRY(launch_lora(a, cfg->max_q_len, static_cast<hipStream_t>(hip_stream)), "adapter kernels");
     return SDV2_OK;
 }

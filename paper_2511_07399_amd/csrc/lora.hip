@@ -22,12 +22,10 @@ struct Tile {
 };
 template <int TOKENS>
 __device__ __forceinline__ bool locate(const LoraArgs& a, int tile, Tile* t) {
-    const int s = find_sequence(a.n_seqs, tile, [&](int i) { return a.q_start[i] / TOKENS + i; });
-    if (s >= a.n_seqs) return false;
-    const int q0 = __builtin_amdgcn_readfirstlane(a.q_start[s]), n = __builtin_amdgcn_readfirstlane(a.q_start[s + 1]) - q0;
-    const int id = __builtin_amdgcn_readfirstlane(a.adapter[s]);
-    if (q0 < 0 || n < 0 || n > a.n_tokens - q0) return false;         // not a batch: touch nothing
-    const int at = (tile - q0 / TOKENS - s) * TOKENS;
+    const Sequence s = sequence_at(a.q_start, a.adapter, a.n_seqs, tile, [](int end, int i) { return end / TOKENS + i; });
+    const int q0 = s.q0, n = s.n, id = s.more;
+    if (s.index >= a.n_seqs || q0 < 0 || n < 0 || n > a.n_tokens - q0) return false;      // (not a batch: touch nothing)
+    const int at = (tile - q0 / TOKENS - s.index) * TOKENS;
     if (at >= n) return false;
     t->first = q0 + at;
     t->count = min(TOKENS, n - at);
@@ -42,10 +40,11 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
     __shared__ f32x4 parts[kDownWaves][RT * NT][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l15 = lane & 15, lk = lane >> 4;
-    const unsigned tile = blockIdx.x / groups;
+    const unsigned rest = blockIdx.x / a.parts, part = blockIdx.x - rest * a.parts, tile = rest / groups;
     Tile t;
     if (!locate<16 * NT>(a, (int)tile, &t) || t.adapter < 0) return;
-    const int rank0 = (int)(blockIdx.x - tile * groups) * (16 * RT);
+    const int rank0 = (int)(rest - tile * groups) * (16 * RT);
+    const float scale = a.scale != nullptr ? a.scale[t.adapter] : 1.0f;
 
     const bf16 *wp[RT], *xp[NT];
 #pragma unroll
@@ -58,9 +57,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // pieces of 64 numbers (a line of 128 bytes in a row); several at once, so that their loads are in flight together
-    constexpr int kAtOnce = RT * NT == 1 ? 5 : RT + NT <= 4 ? 3 : 2;
-    const int pieces = a.K >> 6;
-    for (int p0 = wave; p0 < pieces; p0 += kDownWaves * kAtOnce) {
+    constexpr int kAtOnce = 3;
+    const int all = a.K >> 6, pieces = (int)((long long)all * (part + 1) / a.parts);
+    for (int p0 = (int)((long long)all * part / a.parts) + wave; p0 < pieces; p0 += kDownWaves * kAtOnce) {
         bf16x8 w[kAtOnce][2][RT], x[kAtOnce][2][NT];
 #pragma unroll
         for (int c = 0; c < kAtOnce; ++c) {
@@ -73,6 +72,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
                 for (int j = 0; j < NT; ++j) x[c][h][j] = *reinterpret_cast<const bf16x8*>(xp[j] + at + 32 * h);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);       // (left to itself, the compiler puts each load in front of its product)
 #pragma unroll
         for (int c = 0; c < kAtOnce; ++c) {
             if (p0 + kDownWaves * c >= pieces) break;
@@ -89,13 +89,18 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
 #pragma unroll
         for (int j = 0; j < NT; ++j) parts[wave][i * NT + j][lane] = acc[i][j];
     __syncthreads();
-    const float scale = a.scale != nullptr ? a.scale[t.adapter] : 1.0f;
     for (int b = wave; b < RT * NT; b += kDownWaves) {
         f32x4 u = parts[0][b][lane];
 #pragma unroll
         for (int k = 1; k < kDownWaves; ++k) u += parts[k][b][lane];
         const int rank = rank0 + 16 * (b / NT) + 4 * lk, token = 16 * (b % NT) + l15;      // four ranks of one token
         if (token >= t.count || rank >= a.u_ranks) continue;
+        if (NT == 1) {                       // few tokens: the vector unit's form, 32 bits
+#pragma unroll
+            for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
+            *reinterpret_cast<f32x4*>(static_cast<float*>(a.u) + ((long long)part * a.n_tokens + t.first + token) * a.u_ranks + rank) = u;
+            continue;
+        }
         bf16x4 hi, lo;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -103,48 +108,51 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
             hi[e] = (bf16)v;
             lo[e] = (bf16)(v - (float)hi[e]);
         }
-        bf16* const to = a.u + (long long)(t.first + token) * 2 * a.u_ranks + rank;
+        bf16* const to = static_cast<bf16*>(a.u) + (long long)(t.first + token) * 2 * a.u_ranks + rank;
         *reinterpret_cast<bf16x4*>(to) = hi;
         *reinterpret_cast<bf16x4*>(to + a.u_ranks) = lo;
     }
 }
 
-// Sixteen columns of y or out.
+// A lane's sixteen columns of a block of 64 of y or out: pieces of 16 bytes such that the four lanes of a token have 64 bytes next to each
+// other in each.  Which column of the block instruction m's row r is, goes by that: column(m, r).
 template <typename T>
 struct Sixteen;
 template <>
 struct Sixteen<float> {
     f32x4 x[4];
-    __device__ __forceinline__ void load(const float* p) {
+    static __device__ __forceinline__ int column(int m, int r) { return 16 * m + r; }
+    __device__ __forceinline__ void load(const float* p, int lk) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = reinterpret_cast<const f32x4*>(p)[i];
+        for (int m = 0; m < 4; ++m) x[m] = *reinterpret_cast<const f32x4*>(p + 16 * m + 4 * lk);
     }
-    __device__ __forceinline__ f32x4 four(int i) const { return x[i]; }
-    static __device__ __forceinline__ void store(float* p, const f32x4 (&v)[4]) {
+    __device__ __forceinline__ f32x4 four(int m) const { return x[m]; }
+    static __device__ __forceinline__ void store(float* p, int lk, const f32x4 (&v)[4]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) reinterpret_cast<f32x4*>(p)[i] = v[i];
+        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(p + 16 * m + 4 * lk) = v[m];
     }
 };
 template <>
 struct Sixteen<bf16> {
     bf16x8 x[2];
-    __device__ __forceinline__ void load(const bf16* p) {
-        x[0] = reinterpret_cast<const bf16x8*>(p)[0];
-        x[1] = reinterpret_cast<const bf16x8*>(p)[1];
+    static __device__ __forceinline__ int column(int m, int r) { return 32 * (m >> 1) + 8 * (r >> 2) + 4 * (m & 1) + (r & 3); }
+    __device__ __forceinline__ void load(const bf16* p, int lk) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) x[h] = *reinterpret_cast<const bf16x8*>(p + 32 * h + 8 * lk);
     }
-    __device__ __forceinline__ f32x4 four(int i) const {
+    __device__ __forceinline__ f32x4 four(int m) const {
         f32x4 r;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (float)x[i >> 1][4 * (i & 1) + e];
+        for (int e = 0; e < 4; ++e) r[e] = (float)x[m >> 1][4 * (m & 1) + e];
         return r;
     }
-    static __device__ __forceinline__ void store(bf16* p, const f32x4 (&v)[4]) {
+    static __device__ __forceinline__ void store(bf16* p, int lk, const f32x4 (&v)[4]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             bf16x8 o;
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = (bf16)v[2 * h + (e >> 2)][e & 3];
-            reinterpret_cast<bf16x8*>(p)[h] = o;
+            *reinterpret_cast<bf16x8*>(p + 32 * h + 8 * lk) = o;
         }
     }
 };
@@ -161,65 +169,133 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
     if (!locate<TOKENS>(a, (int)tile, &t)) return;
     const T* const y = static_cast<const T*>(a.y);
     T* const out = static_cast<T*>(a.out);
-    if (t.adapter < 0) {
-        if (a.y == a.out) return;
-        for (int i = 0; i < t.count; i += 16)
+    constexpr int NG = TOKENS / 16;                           // sixteens of tokens: their loads are in flight together
+    Sixteen<T> v[NG][NB];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const int n = (block0 + b) * 64 + 16 * lk;
-                if (i + l15 >= t.count || block0 + b >= blocks) continue;
-                Sixteen<T> v;
-                v.load(y + (long long)(t.first + i + l15) * a.y_stride + n);
-                const f32x4 same[4] = {v.four(0), v.four(1), v.four(2), v.four(3)};
-                Sixteen<T>::store(out + (long long)(t.first + i + l15) * a.out_stride + n, same);
-            }
-        return;
-    }
-    // row r of instruction m is column 16 (r / 4) + 4 m + r % 4 of the block
-    const bf16x8 none = {};
-    bf16x8 w[NB][4][KS];
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            const int n = min(block0 + b, blocks - 1) * 64 + 16 * (l15 >> 2) + 4 * m + (l15 & 3);
-            const bf16* const p = a.b + ((long long)t.adapter * a.N + n) * a.rank;
-#pragma unroll
-            for (int k = 0; k < KS; ++k) w[b][m][k] = 32 * k + 8 * lk < a.rank ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
-        }
-    for (int i = 0; i < t.count; i += 16) {
-        const bool live = i + l15 < t.count;
-        const long long row = t.first + min(i + l15, t.count - 1);
-        Sixteen<T> v[NB];
+    for (int g = 0; g < NG; ++g)
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-            if (live) v[b].load(y + row * a.y_stride + min(block0 + b, blocks - 1) * 64 + 16 * lk);
-        bf16x8 u[2][KS];
+            if (16 * g + l15 < t.count)
+                v[g][b].load(y + (long long)(t.first + 16 * g + l15) * a.y_stride + min(block0 + b, blocks - 1) * 64, lk);
+    bf16x8 w[NB][4][KS], u[NG][2][KS];
+    if (t.adapter >= 0) {
+        const bf16x8 none = {};
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int k = 0; k < KS; ++k) u[h][k] = *reinterpret_cast<const bf16x8*>(a.u + (row * 2 + h) * a.u_ranks + 32 * k + 8 * lk);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            f32x4 acc[4];
+                for (int k = 0; k < KS; ++k) {
+                    const bf16* const p = static_cast<const bf16*>(a.u) + ((t.first + min(16 * g + l15, t.count - 1)) * 2ll + h) * a.u_ranks;
+                    u[g][h][k] = 32 * k + 8 * lk < a.u_ranks ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
+                }
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[m] = v[b].four(m);
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) {
+                const bf16* const p = a.b + ((long long)t.adapter * a.N + min(block0 + b, blocks - 1) * 64 + Sixteen<T>::column(m, l15)) * a.rank;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) w[b][m][k] = 32 * k + 8 * lk < a.rank ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
+            }
+    } else if (a.y == a.out) {
+        return;
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) {
+        const bool live = 16 * g + l15 < t.count;
+        const long long row = t.first + min(16 * g + l15, t.count - 1);
+        f32x4 acc[NB][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int m = 0; m < 4; ++m) acc[b][m] = v[g][b].four(m);
+        if (t.adapter >= 0) {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[b][m][k], u[h][k], acc[m], 0, 0, 0);
-            if (live && block0 + b < blocks) Sixteen<T>::store(out + row * a.out_stride + (block0 + b) * 64 + 16 * lk, acc);
+                    for (int b = 0; b < NB; ++b)
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) acc[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[b][m][k], u[g][h][k], acc[b][m], 0, 0, 0);
         }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+            if (live && block0 + b < blocks) Sixteen<T>::store(out + row * a.out_stride + (block0 + b) * 64, lk, acc[b]);
     }
 }
 
-template <typename T, int NB, int TOKENS>
-void launch_up(const LoraArgs& a, hipStream_t s) {
+// Few tokens of a sequence: on the vector unit, where a tile of sixteen tokens would mostly be empty and its accumulators cost the places
+// of other waves.  A lane has two columns, 16 CH ranks of which it holds at once; u, summed over the parts of K, goes round by
+// readlane.  64 tokens of rank 16 over 15 360 columns: 12.5 us on the matrix instructions, 7.8 with one part of K, so.
+template <typename T, int CH>
+__global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned groups) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tile = blockIdx.x / groups;
+    const int n = ((int)(blockIdx.x - tile * groups) * 4 + wave) * 128 + 2 * lane;
+    Tile t;
+    if (!locate<16>(a, (int)tile, &t)) return;
+    typedef T T2 __attribute__((ext_vector_type(2)));
+    const bool live = n < a.N;
+    const int at = min(n, a.N - 2);
+    const T* const y = static_cast<const T*>(a.y);
+    T* const out = static_cast<T*>(a.out);
+    const bool adapted = t.adapter >= 0;
+    if (!adapted && a.y == a.out) return;
+    const bf16* const rows = a.b + ((long long)max(t.adapter, 0) * a.N + at) * a.rank;
+    bf16x8 w[2][CH][2];
+    auto fetch = [&](int r0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = r0 + 16 * c + 8 * h;
+                    w[i][c][h] = *reinterpret_cast<const bf16x8*>(rows + (long long)i * a.rank + min(r, a.rank - 8));       // past the end: times u = 0
+                }
+    };
+    const bool once = a.rank <= 16 * CH;
+    if (adapted && once) fetch(0);
+    for (int i = 0; i < t.count; ++i) {
+        const long long row = t.first + i;
+        const T2 own = *reinterpret_cast<const T2*>(y + row * a.y_stride + at);
+        float x0 = (float)own[0], x1 = (float)own[1];
+        if (adapted)
+            for (int r0 = 0; r0 < a.rank; r0 += 16 * CH) {
+                if (!once) fetch(r0);
+                const int r = r0 + (lane & (16 * CH - 1));
+                float u = 0.0f;
+                for (int p = 0; p < a.parts; ++p)
+                    u += r < a.u_ranks ? static_cast<const float*>(a.u)[((long long)p * a.n_tokens + row) * a.u_ranks + r] : 0.0f;
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const float ue = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), 16 * c + e));
+                        x0 = fmaf(ue, (float)w[0][c][e >> 3][e & 7], x0);
+                        x1 = fmaf(ue, (float)w[1][c][e >> 3][e & 7], x1);
+                    }
+            }
+        if (live) *reinterpret_cast<T2*>(out + row * a.out_stride + n) = T2{(T)x0, (T)x1};
+    }
+}
+
+template <typename T>
+void launch_up(const LoraArgs& a, bool few, hipStream_t s) {
+    if (few) {
+        const unsigned groups = (unsigned)(a.N + 511) / 512;
+        const dim3 grid(groups * (unsigned)(a.n_tokens / 16 + a.n_seqs));
+        if (a.rank <= 16) hipLaunchKernelGGL((lora_up_few_kernel<T, 1>), grid, dim3(256), 0, s, a, groups);
+        else if (a.rank <= 32) hipLaunchKernelGGL((lora_up_few_kernel<T, 2>), grid, dim3(256), 0, s, a, groups);
+        else hipLaunchKernelGGL((lora_up_few_kernel<T, 4>), grid, dim3(256), 0, s, a, groups);
+        return;
+    }
+    constexpr int NB = 1, TOKENS = 32;
     const unsigned groups = (unsigned)(a.N / 64 + 4 * NB - 1) / (4 * NB);
     const dim3 grid(groups * (unsigned)(a.n_tokens / TOKENS + a.n_seqs));
-    switch (a.u_ranks / 32) {
+    switch ((a.u_ranks + 31) / 32) {
         case 1: hipLaunchKernelGGL((lora_up_kernel<T, 1, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
         case 2: hipLaunchKernelGGL((lora_up_kernel<T, 2, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
         case 3: hipLaunchKernelGGL((lora_up_kernel<T, 3, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
@@ -229,10 +305,16 @@ void launch_up(const LoraArgs& a, hipStream_t s) {
 template <int NT, int RT>
 void launch_down(const LoraArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)(a.u_ranks + 16 * RT - 1) / (16 * RT);
-    hipLaunchKernelGGL((lora_down_kernel<NT, RT>), dim3(groups * (unsigned)(a.n_tokens / (16 * NT) + a.n_seqs)), dim3(64 * kDownWaves), 0, s, a, groups);
+    hipLaunchKernelGGL((lora_down_kernel<NT, RT>), dim3(groups * a.parts * (unsigned)(a.n_tokens / (16 * NT) + a.n_seqs)), dim3(64 * kDownWaves), 0, s, a, groups);
 }
 
 }  // namespace
+
+int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
+    if (max_q_len > 16) return 1;
+    const int workgroups = max(n_tokens / 16, n_seqs) * ((rank + 15) / 16);
+    return max(1, min(min(kUnits / workgroups, K / 1024), 4));
+}
 
 hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
     const bool few = max_q_len <= 16;
@@ -241,8 +323,8 @@ hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
     else launch_down<2, 4>(a, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.fp32) few ? launch_up<float, 2, 16>(a, s) : launch_up<float, 1, 64>(a, s);
-    else few ? launch_up<bf16, 2, 16>(a, s) : launch_up<bf16, 1, 64>(a, s);
+    if (a.fp32) launch_up<float>(a, few, s);
+    else launch_up<bf16>(a, few, s);
     return hipGetLastError();
 }
 

@@ -77,13 +77,13 @@ struct Work {
 // Row tiles are numbered without a table: those of sequence s start at floor(q_start[s] group / tile) + s, which leaves each sequence
 // at least as many numbers as it has tiles.  False: a number that no tile has.
 __device__ __forceinline__ bool locate(const PagedAttnArgs& a, int tile_rows, int tile, Work* w) {
-    auto start = [&](int s) { return (int)((long long)a.batch.q_start[s] * a.group / tile_rows) + s; };
-    w->seq = find_sequence(a.batch.n_seqs, tile, start);
+    const Sequence s = sequence_at(a.batch.q_start, a.batch.kv_len, a.batch.n_seqs, tile,
+                                   [&](int end, int i) { return (int)((long long)end * a.group / tile_rows) + i; });
+    w->seq = s.index;
     if (w->seq >= a.batch.n_seqs) return false;
-    w->q0 = __builtin_amdgcn_readfirstlane(a.batch.q_start[w->seq]);
-    w->n = __builtin_amdgcn_readfirstlane(a.batch.q_start[w->seq + 1]) - w->q0;
-    const long long room = (long long)a.batch.table_stride << a.batch.page_shift;
-    w->kv_len = (int)min((long long)__builtin_amdgcn_readfirstlane(a.batch.kv_len[w->seq]), room);
+    w->q0 = s.q0;
+    w->n = s.n;
+    w->kv_len = (int)min((long long)s.more, (long long)a.batch.table_stride << a.batch.page_shift);
     if (w->q0 < 0 || w->n < 0 || w->n > a.batch.n_tokens - w->q0) return false;      // not a batch: touch nothing
     w->rows = w->n * a.group;
     w->row0 = (tile - (int)((long long)w->q0 * a.group / tile_rows) - w->seq) * tile_rows;

@@ -32,8 +32,31 @@ __device__ __forceinline__ int find_sequence(int n_seqs, int t, F&& ends) {
     }
     return __builtin_amdgcn_readfirstlane(first);
 }
-__device__ __forceinline__ int sequence_of_row(const RaggedArgs& b, int t) {
-    return find_sequence(b.n_seqs, t, [&](int s) { return b.q_start[s]; });
+
+// That sequence with its rows and one more number of it.  Up to 64 sequences are looked at by a lane each, which fetches all of
+// it at once: a second round of loads behind the first is 0.7 us of a launch of a few.
+struct Sequence {
+    int index, q0, n, more;
+};
+template <typename F>
+__device__ __forceinline__ Sequence sequence_at(const int* q_start, const int* more, int n_seqs, int t, F&& ends) {
+    Sequence s;
+    if (n_seqs <= 64) {
+        const int lane = threadIdx.x & 63, i = min(lane, n_seqs - 1);
+        const int first = q_start[i], last = q_start[i + 1], other = more[i];
+        s.index = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < n_seqs && ends(last, i + 1) <= t));
+        const int at = min(s.index, n_seqs - 1);
+        s.q0 = __builtin_amdgcn_readlane(first, at);
+        s.n = __builtin_amdgcn_readlane(last, at) - s.q0;
+        s.more = __builtin_amdgcn_readlane(other, at);
+        return s;
+    }
+    s.index = find_sequence(n_seqs, t, [&](int i) { return ends(q_start[i], i); });
+    const int at = min(s.index, n_seqs - 1);
+    s.q0 = __builtin_amdgcn_readfirstlane(q_start[at]);
+    s.n = __builtin_amdgcn_readfirstlane(q_start[at + 1]) - s.q0;
+    s.more = __builtin_amdgcn_readfirstlane(more[at]);
+    return s;
 }
 
 // Keys that a row may see: j < end, and j >= low or j < sink.
@@ -126,9 +149,12 @@ struct LoraArgs {
     void* out;
     long long x_stride, y_stride, out_stride;
     int n_seqs, n_tokens, K, N, rank, n_adapters, fp32;
-    bf16* u;                          // scale x A^T: [n_tokens][high, low][u_ranks]
-    int u_ranks;                      // rank rounded up to 32
+    void* u;                          // scale x A^T: [n_tokens][high, low][u_ranks] bf16; few tokens, K in parts: [parts][n_tokens][u_ranks] fp32
+    int u_ranks;                      // rank rounded up to 16
+    int parts;
 };
+// parts of K: n_seqs, n_tokens, max_q_len, K, rank
+int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank);
 hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s);
 
 }  // namespace sdv2

@@ -65,12 +65,12 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnArgs a, int waves_per_row
     // where the row's key and value go: its sequence, its place there, the page
     long long slot = -1;                                       // page * kv_heads * P + slot in the page
     if (PAGES) {
-        const int s = sequence_of_row(a.batch, row);
-        if (s >= a.batch.n_seqs) return;                       // behind the last sequence: nothing of it is written
-        const int at = a.batch.kv_len[s] - a.batch.q_start[s + 1] + row;
+        const Sequence s = sequence_at(a.batch.q_start, a.batch.kv_len, a.batch.n_seqs, row, [](int end, int) { return end; });
+        if (s.index >= a.batch.n_seqs) return;                 // behind the last sequence: nothing of it is written
+        const int at = s.more - s.n + row - s.q0;
         const int entry = at >> a.batch.page_shift;
         if (at >= 0 && entry < a.batch.table_stride) {
-            const int page = a.batch.table[(long long)s * a.batch.table_stride + entry];
+            const int page = a.batch.table[(long long)s.index * a.batch.table_stride + entry];
             if ((unsigned)page < (unsigned)a.batch.n_pages)
                 slot = (((long long)page * a.k_heads) << a.batch.page_shift) + (at & ((1 << a.batch.page_shift) - 1));
         }
