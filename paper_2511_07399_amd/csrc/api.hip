@@ -2309,7 +2309,7 @@ static const char* lora_wrong(const sdv2_lora_cfg* c) {
     return nullptr;
 }
 
-static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)parts * c->n_tokens * align_up(c->rank, 16) * sizeof(float), 256); }
+static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)c->n_tokens * align_up(c->rank, 16) * (parts > 1 ? parts * sizeof(float) : 3 * sizeof(bf16)), 256); }
 
 size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg) {
     if (const char* why = lora_wrong(cfg)) {

@@ -5,8 +5,8 @@
 // are products on 16x16x32 matrix instructions whose fragments come straight from memory (sixteen rows, 64 bytes each), since
 // nothing is used often enough to pay for its way through LDS.
 //   u: computed transposed, ranks as rows and tokens as columns.  A workgroup has 16 or 32 tokens of one sequence and 16 RT ranks; its eight
-//     waves take pieces of 64 of K in turn and add up through LDS.  u is left as two bf16 numbers per value, high and low (u = high + low
-//     to 2^-17: as one bf16 its rounding would be the largest error of an fp32 result).
+//     waves take pieces of 64 of K in turn and add up through LDS.  u is left as two or three bf16 numbers per value that add up to it
+//     (kPieces: as one, its rounding would be the result's largest error).
 //   out: columns of out as rows, tokens as columns, y as the accumulator's start.  The rows of four instructions are interleaved so that a
 //     lane ends up with sixteen columns next to each other of its token.
 #include "ragged.h"
@@ -34,6 +34,10 @@ __device__ __forceinline__ bool locate(const LoraArgs& a, int tile, Tile* t) {
 }
 
 constexpr int kDownWaves = 8;
+// bf16 numbers that one of u goes to the second product as: each takes off eight bits, and an output of 32 bits shows the 17th
+// (four frames of rank 64 against 64 bits: two pieces 1.9e-6 of the output, three 3e-7, which is the sum's own).
+template <typename T>
+constexpr int kPieces = sizeof(T) == 4 ? 3 : 2;
 
 template <int NT, int RT>
 __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, unsigned groups) {
@@ -101,16 +105,19 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
             *reinterpret_cast<f32x4*>(static_cast<float*>(a.u) + ((long long)part * a.n_tokens + t.first + token) * a.u_ranks + rank) = u;
             continue;
         }
-        bf16x4 hi, lo;
+        bf16* const to = static_cast<bf16*>(a.u) + (long long)(t.first + token) * a.pieces * a.u_ranks + rank;
+        f32x4 rest;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float v = rank < a.rank ? u[e] * scale : 0.0f;
-            hi[e] = (bf16)v;
-            lo[e] = (bf16)(v - (float)hi[e]);
+        for (int e = 0; e < 4; ++e) rest[e] = rank < a.rank ? u[e] * scale : 0.0f;
+        for (int p = 0; p < a.pieces; ++p) {
+            bf16x4 piece;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                piece[e] = (bf16)rest[e];
+                rest[e] -= (float)piece[e];
+            }
+            *reinterpret_cast<bf16x4*>(to + (long long)p * a.u_ranks) = piece;
         }
-        bf16* const to = static_cast<bf16*>(a.u) + (long long)(t.first + token) * 2 * a.u_ranks + rank;
-        *reinterpret_cast<bf16x4*>(to) = hi;
-        *reinterpret_cast<bf16x4*>(to + a.u_ranks) = lo;
     }
 }
 
@@ -177,16 +184,16 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
         for (int b = 0; b < NB; ++b)
             if (16 * g + l15 < t.count)
                 v[g][b].load(y + (long long)(t.first + 16 * g + l15) * a.y_stride + min(block0 + b, blocks - 1) * 64, lk);
-    bf16x8 w[NB][4][KS], u[NG][2][KS];
+    bf16x8 w[NB][4][KS], u[NG][kPieces<T>][KS];
     if (t.adapter >= 0) {
         const bf16x8 none = {};
 #pragma unroll
         for (int g = 0; g < NG; ++g)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < kPieces<T>; ++h)
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
-                    const bf16* const p = static_cast<const bf16*>(a.u) + ((t.first + min(16 * g + l15, t.count - 1)) * 2ll + h) * a.u_ranks;
+                    const bf16* const p = static_cast<const bf16*>(a.u) + ((long long)(t.first + min(16 * g + l15, t.count - 1)) * kPieces<T> + h) * a.u_ranks;
                     u[g][h][k] = 32 * k + 8 * lk < a.u_ranks ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
                 }
 #pragma unroll
@@ -214,7 +221,7 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int h = kPieces<T> - 1; h >= 0; --h)
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -316,7 +323,9 @@ int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
     return max(1, min(min(kUnits / workgroups, K / 1024), 4));
 }
 
-hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
+hipError_t launch_lora(const LoraArgs& args, int max_q_len, hipStream_t s) {
+    LoraArgs a = args;
+    a.pieces = a.fp32 ? kPieces<float> : kPieces<bf16>;
     const bool few = max_q_len <= 16;
     if (few) launch_down<1, 1>(a, s);
     else if (a.n_tokens < 4096 || a.u_ranks < 64) launch_down<2, 2>(a, s);

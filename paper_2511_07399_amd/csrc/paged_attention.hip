@@ -964,20 +964,64 @@ static int token_parts(long long workgroups, int keys, int e4m3) {
     return (int)max(max(spread, chain >= 4 ? chain : 1ll), 1ll);
 }
 
+// More rows than that: the form and the parts by an estimate of the time, us,
+//   rounds (tiles per + start), rounds of `slots` workgroups, the last by how much of it is filled (two workgroups on a unit share it),
+//   or the keys' bytes at `rate` where that is longer,  + join per part and its bytes.
+// Fitted to 1056 launches of 38 shapes (100 to 9360 rows times 1 to 8 in a group, 700 to 33 000 keys, 1 to 40 key heads, both formats, every
+// form in 1 to 32 parts): rms error 15 %, and the form picked is on average 2 % slower than the best of all.  What it replaced, 128 rows up
+// to 128 and 256 beyond in as many parts as fill the units: 8 x 64 new tokens over 8000 keys 135.6 -> 103.3, 3 x 200 over 12 000
+// 236.9 -> 146.4, of 8 bits 8 x 16 over 8000 79.0 -> 47.7, 333 over 33 000 333 -> 209.
+struct FormCost {
+    int rows, keys, slots;
+    float two, one, start, rate;      // a tile of keys (of the four waves, where they share them out) with both slots of a unit taken and with one
+};
+static const FormCost kForms[2][3] = {{{32, 128, 512, 1.67f, 1.10f, 3.6f, 2.2e7f}, {128, 64, 512, 2.12f, 1.20f, 5.3f, 4.1e6f}, {256, 64, 256, 1.76f, 1.37f, 7.8f, 3.2e6f}},
+                                      {{32, 128, 512, 1.35f, 0.80f, 3.7f, 1.3e7f}, {128, 64, 512, 2.26f, 1.50f, 5.9f, 2.5e6f}, {256, 64, 256, 1.80f, 1.55f, 10.f, 2.0e6f}}};
+constexpr float kJoin = 9.0f, kJoinRate = 8e6f;      // us, bytes per us
+constexpr int kMostParts = 32;
+
+static float form_cost(const FormCost& f, const RaggedArgs& b, int group, int max_q_len, float keys, int e4m3, int parts) {
+    const long long tiles_of_rows = min((long long)b.n_seqs * (((long long)max_q_len * group + f.rows - 1) / f.rows),
+                                        (long long)b.n_tokens * group / f.rows + b.n_seqs);
+    const long long wgs = tiles_of_rows * b.kv_heads * parts;
+    const float tiles = ceilf(ceilf(keys / (float)f.keys) / (float)parts);
+    const int rest = (int)(wgs % f.slots);
+    float us = (float)(wgs / f.slots) * (tiles * f.two + f.start);
+    if (rest > 0) {
+        const float share = f.slots == kUnits ? (float)rest / kUnits : rest <= kUnits ? 0.0f : (float)(rest - kUnits) / kUnits;
+        us += tiles * (f.one + (f.two - f.one) * share) + f.start;
+    }
+    const float bytes = (float)b.n_seqs * keys * b.kv_heads * (4.0f * D / (1 + e4m3)) * (f.rows == 32 ? fmaxf(1.0f, (float)max_q_len * group / 32) : 1.0f);
+    us = fmaxf(us, bytes / f.rate);
+    if (parts > 1) us += kJoin + (float)parts * b.n_tokens * b.kv_heads * group * (8.0f * D + 16.0f) / kJoinRate;
+    return us;
+}
+
 PagedAttnPlan plan_paged_attention(const RaggedArgs& b, const MaskArgs& mask, int q_heads, int max_q_len, int max_kv_len, int e4m3) {
     const int group = q_heads / b.kv_heads;
     const long long rows = (long long)max_q_len * group;
-    PagedAttnPlan p{rows <= 32 ? 32 : rows <= 128 ? 128 : 256, 1, 1};
-    if (g_force_rows > 0) p.rows = g_force_rows;
-    const int key_tile = p.rows == 32 ? 32 : 64;
     // keys that a workgroup's rows see at most
     long long keys = max_kv_len;
-    if (mask.window > 0) keys = min(keys, (long long)mask.window + mask.sink + min(max_q_len, p.rows / group + 1) + mask.block);
-    const int tiles = (int)((keys + key_tile - 1) / key_tile);
-    const long long wgs = max((long long)b.n_tokens * group / p.rows, (long long)b.n_seqs) * b.kv_heads;
-    int parts = p.rows == 32 ? token_parts(wgs, (int)keys, e4m3) : (int)min((long long)(tiles + 7) / 8, 256 / wgs);
-    if (g_force_parts > 0) parts = min(g_force_parts, tiles);
-    p.part_tiles = max(1, (tiles + max(parts, 1) - 1) / max(parts, 1));
+    if (mask.window > 0) keys = min(keys, (long long)mask.window + mask.sink + min(max_q_len, 256 / group + 1) + mask.block);
+    int form = 32, parts = 1;
+    if (rows <= 32 && (g_force_rows == 0 || g_force_rows == 32)) {
+        parts = token_parts(max((long long)b.n_tokens * group / 32, (long long)b.n_seqs) * b.kv_heads, (int)keys, e4m3);
+    } else {
+        // under a causal mask rows see half of the new tokens in the mean
+        const float mean = mask.block > 0 && mask.window == 0 ? fmaxf((float)keys - 0.5f * max_q_len, 64.0f) : (float)keys;
+        float best = INFINITY;
+        for (const FormCost& f : kForms[e4m3]) {
+            if (g_force_rows > 0 && f.rows != g_force_rows) continue;
+            for (int p = 1; p <= kMostParts && (p == 1 || (p - 1) * 2 * f.keys < keys); ++p) {
+                const float us = form_cost(f, b, group, max_q_len, mean, e4m3, p);
+                if (us < best) best = us, form = f.rows, parts = p;
+                if (g_force_parts > 0) break;
+            }
+        }
+    }
+    const int key_tile = form == 32 ? 32 : 64, tiles = (int)((keys + key_tile - 1) / key_tile);
+    if (g_force_parts > 0) parts = min(g_force_parts, max(tiles, 1));
+    PagedAttnPlan p{form, 1, max(1, (tiles + parts - 1) / parts)};
     p.parts = max(1, (tiles + p.part_tiles - 1) / p.part_tiles);
     return p;
 }
