@@ -862,9 +862,18 @@ def _turned(t, out, gain, dev, rows):
     """The six arguments of rows that are normed and turned."""
     if t is None:
         return _NO_ROWS
-    p, stride, heads = _heads(t, dev, rows)
-    po, out_stride = _rows(out, dev, heads * HEAD_DIM, rows)
-    return p, stride, heads, _gain(gain, dev), po, out_stride
+    n, w = t.shape
+    s0, s1 = t.stride()
+    o0, o1 = out.stride()
+    assert n == rows and w % HEAD_DIM == 0 and w > 0 and s1 == 1 and t.dtype is _BF16 and t.get_device() == dev, \
+        "expected %d rows of heads of 128 bfloat16 on the current device" % rows
+    assert out.shape == (n, w) and o1 == 1 and out.dtype is _BF16 and out.get_device() == dev, "outputs have the shape and type of the rows"
+    if n == 1:
+        s0 = o0 = w                                          # the stride of a single row says nothing, and may be anything
+    if gain is not None:
+        assert gain.numel() == HEAD_DIM and gain.dtype is _F32 and gain.get_device() == dev and gain.is_contiguous(), "a gain has 128 float32 numbers"
+        gain = gain.data_ptr()
+    return t.data_ptr(), s0, w // HEAD_DIM, gain, out.data_ptr(), o0
 
 
 def qk_norm_rope(rope, positions, q, q_out, g_q=None, k=None, k_out=None, g_k=None):

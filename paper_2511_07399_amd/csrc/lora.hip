@@ -184,18 +184,9 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
         for (int b = 0; b < NB; ++b)
             if (16 * g + l15 < t.count)
                 v[g][b].load(y + (long long)(t.first + 16 * g + l15) * a.y_stride + min(block0 + b, blocks - 1) * 64, lk);
-    bf16x8 w[NB][4][KS], u[NG][kPieces<T>][KS];
+    bf16x8 w[NB][4][KS], u[kPieces<T>][KS];
     if (t.adapter >= 0) {
         const bf16x8 none = {};
-#pragma unroll
-        for (int g = 0; g < NG; ++g)
-#pragma unroll
-            for (int h = 0; h < kPieces<T>; ++h)
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16* const p = static_cast<const bf16*>(a.u) + ((long long)(t.first + min(16 * g + l15, t.count - 1)) * kPieces<T> + h) * a.u_ranks;
-                    u[g][h][k] = 32 * k + 8 * lk < a.u_ranks ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
-                }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -218,6 +209,14 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
 #pragma unroll
             for (int m = 0; m < 4; ++m) acc[b][m] = v[g][b].four(m);
         if (t.adapter >= 0) {
+            const bf16x8 none = {};
+#pragma unroll
+            for (int h = 0; h < kPieces<T>; ++h)
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const bf16* const p = static_cast<const bf16*>(a.u) + ((long long)(t.first + min(16 * g + l15, t.count - 1)) * kPieces<T> + h) * a.u_ranks;
+                    u[h][k] = 32 * k + 8 * lk < a.u_ranks ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
+                }
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -225,7 +224,7 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
 #pragma unroll
                     for (int b = 0; b < NB; ++b)
 #pragma unroll
-                        for (int m = 0; m < 4; ++m) acc[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[b][m][k], u[g][h][k], acc[b][m], 0, 0, 0);
+                        for (int m = 0; m < 4; ++m) acc[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[b][m][k], u[h][k], acc[b][m], 0, 0, 0);
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
