@@ -955,11 +955,11 @@ void set_paged_overrides(int rows, int parts) {
 // after the units with one; many small parts even that out and even out the lengths, which only the device knows.  A part costs a
 // workgroup's start (4 us) and the join's reading: it is worth 512 keys (8-bit pages, half the bytes: 1024).  With less than a
 // workgroup per unit the chain of a workgroup's tiles is the time, and 128 keys, one tile a wave, are worth a part.  us, bf16, 8 key
-// heads, equal lengths, this rule / best number of parts: 64 x 7584 keys 346 / 335, 32 x 12 000 276 / 270, 32 x 700 24.9 / 23.3, 12 x 3000
-// 38.7 / 35.0, 4 x 3000 17.3 / 17.3, 4 x 700 11.7 / 11.7, 1 x 12 000 17.5 / 17.4, 1 x 3000 12.4 / 12.4.  64 x 1 to 16 000: 367 / 363, one
-// part 387.
+// heads, equal lengths, this rule / best number of parts: 64 x 7584 keys 351 / 335, 32 x 12 000 282 / 270, 32 x 700 24.9 / 23.3, 12 x 3000
+// 38.7 / 35.0, 4 x 3000 17.3 / 17.3, 4 x 700 11.7 / 11.7, 1 x 12 000 17.5 / 17.4, 1 x 3000 12.4 / 12.4.  64 x 1 to 16 000: 363 / 363, one
+// part 387; of 8 bits 194 / 194, one part 214.
 static int token_parts(long long workgroups, int keys, int e4m3) {
-    const long long spread = min((2048 + workgroups - 1) / workgroups, (long long)(keys / (e4m3 ? 1024 : 512)));
+    const long long spread = min((4096 + workgroups - 1) / workgroups, (long long)(keys / (e4m3 ? 1024 : 512)));
     const long long chain = min(kUnits / workgroups, (long long)(keys / 128));
     return (int)max(max(spread, chain >= 4 ? chain : 1ll), 1ll);
 }
