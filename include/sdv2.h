@@ -589,7 +589,7 @@ typedef struct sdv2_paged_cfg {
     int32_t page_tokens;          /* 16, 32, 64, 128 or 256 */
     int32_t n_pages;              /* > 0 */
     int32_t format;               /* SDV2_PAGES_BF16 or SDV2_PAGES_E4M3 */
-    float k_scale, v_scale;       /* > 0; 1 for bf16 */
+    float k_scale, v_scale;       /* 1e-30 .. 1e30; 1 for bf16 */
 } sdv2_paged_cfg;
 
 /* Bytes of EACH of the two pools (0 on a bad cfg). */
@@ -654,7 +654,7 @@ int32_t sdv2_paged_attention(const sdv2_paged_cfg* cfg, const void* k_pages_dev,
  *     out[t] = y[t] + scale[i] (x[t] A_i^T) B_i^T,   i = adapter[s] of the row's sequence s;
  *   an id outside [0, n_adapters) is no adapter: out[t] = y[t].  x: bf16 rows of K; A: bf16 [n_adapters][rank][K]; B: bf16
  *   [n_adapters][N][rank]; scale: dev fp32 [n_adapters] or NULL (1); adapter: dev int32 [n_seqs]; q_start as in a ragged batch.
- *   y, out: rows of N, bf16 (out_fp32 = 0) or fp32 (1); out may be y.  Sums are held in 32 bits; x A^T goes to the second product in
+ *   y, out: rows of N, bf16 (out_fp32 = 0) or fp32 (1); out may be y, and overlaps nothing else that is read.  Sums are held in 32 bits; x A^T goes to the second product in
  *   32 bits, or as two (bf16 rows) or three (fp32 rows) bf16 numbers that add up to it.  K and N multiples of 64, rank a multiple of 8 up to 128.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct sdv2_lora_cfg {

@@ -2076,7 +2076,7 @@ const char* paged_cfg_wrong(const sdv2_paged_cfg* c) {
     if (c->page_tokens < 16 || c->page_tokens > 256 || (c->page_tokens & (c->page_tokens - 1))) return "page_tokens must be 16, 32, 64, 128 or 256";
     if (c->n_pages <= 0) return "n_pages must be positive";
     if (c->format != SDV2_PAGES_BF16 && c->format != SDV2_PAGES_E4M3) return "unknown page format";
-    if (!(c->k_scale > 0.0f) || !(c->v_scale > 0.0f) || isinf(c->k_scale) || isinf(c->v_scale)) return "scales must be positive";
+    if (!(c->k_scale >= 1e-30f) || !(c->v_scale >= 1e-30f) || c->k_scale > 1e30f || c->v_scale > 1e30f) return "scales must lie in 1e-30 .. 1e30";
     if (c->format == SDV2_PAGES_BF16 && (c->k_scale != 1.0f || c->v_scale != 1.0f)) return "bf16 pages have no scale";
     return nullptr;
 }
@@ -2157,7 +2157,7 @@ int32_t sdv2_qk_norm_rope(const sdv2_rope_cfg* rope, int32_t n_tokens, const int
     if (!rope) return fail(SDV2_INVALID_ARG, "rope is null");
     if (const char* why = rope_wrong(rope)) return fail(SDV2_INVALID_ARG, "%s", why);
     if (n_tokens < 0 || q_heads < 0 || k_heads < 0 || q_heads + (int64_t)k_heads == 0) return fail(SDV2_INVALID_ARG, "bad n_tokens or heads");
-    if ((int64_t)n_tokens * (q_heads + (int64_t)k_heads) > kMostRowHeads) return fail(SDV2_INVALID_ARG, "more than 2^26 heads of rows");
+    if (n_tokens > (1 << 25) || (int64_t)n_tokens * (q_heads + (int64_t)k_heads) > kMostRowHeads) return fail(SDV2_INVALID_ARG, "more than 2^26 heads of rows");
     if (n_tokens == 0) return SDV2_OK;
     if (rope->axes > 0 && !pos_dev) return fail(SDV2_INVALID_ARG, "positions are null");
     if (q_heads > 0)
@@ -2236,6 +2236,7 @@ static const char* paged_attention_wrong(const sdv2_paged_cfg* cfg, const sdv2_r
     if (mask->scale != mask->scale || isinf(mask->scale)) return "scale is not finite";
     if (q_heads <= 0 || q_heads % cfg->kv_heads) return "q_heads must be a multiple of kv_heads";
     if ((int64_t)batch->n_tokens * q_heads > kMostRowHeads) return "more than 2^26 heads of rows";
+    if ((int64_t)batch->n_seqs * cfg->kv_heads > ((int64_t)1 << 21)) return "more than 2^21 key heads of sequences";
     return nullptr;
 }
 

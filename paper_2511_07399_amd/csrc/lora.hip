@@ -26,7 +26,7 @@ __device__ __forceinline__ bool locate(const LoraArgs& a, int tile, Tile* t) {
     const int q0 = s.q0, n = s.n, id = s.more;
     if (s.index >= a.n_seqs || q0 < 0 || n < 0 || n > a.n_tokens - q0) return false;      // (not a batch: touch nothing)
     const int at = (tile - q0 / TOKENS - s.index) * TOKENS;
-    if (at >= n) return false;
+    if (at < 0 || at >= n) return false;
     t->first = q0 + at;
     t->count = min(TOKENS, n - at);
     t->adapter = (unsigned)id < (unsigned)a.n_adapters ? id : -1;

@@ -46,7 +46,8 @@ __device__ __forceinline__ float max2(float a, float b) {
     asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
     return r;
 }
-// Largest of a block's sixteen scores and of the partner lane's (the same row's other sixteen keys); NaN gives way.
+// Largest of a block's sixteen scores and of the partner lane's (the same row's other sixteen keys); NaN gives way.  (Written as
+// instructions, which wait for no product: the caller has read the scores in ordinary code before.)
 __device__ __forceinline__ float block_max(const f32x16& s) {
     float m[4];
 #pragma unroll
@@ -87,7 +88,7 @@ __device__ __forceinline__ bool locate(const PagedAttnArgs& a, int tile_rows, in
     if (w->q0 < 0 || w->n < 0 || w->n > a.batch.n_tokens - w->q0) return false;      // not a batch: touch nothing
     w->rows = w->n * a.group;
     w->row0 = (tile - (int)((long long)w->q0 * a.group / tile_rows) - w->seq) * tile_rows;
-    return w->row0 < w->rows;
+    return w->row0 >= 0 && w->row0 < w->rows;
 }
 
 // The key tiles that a run of rows sees, in order: those of the sink, then those from the window on.
@@ -979,6 +980,7 @@ static const FormCost kForms[2][3] = {{{32, 128, 512, 1.67f, 1.10f, 3.6f, 2.2e7f
                                       {{32, 128, 512, 1.35f, 0.80f, 3.7f, 1.3e7f}, {128, 64, 512, 2.26f, 1.50f, 5.9f, 2.5e6f}, {256, 64, 256, 1.80f, 1.55f, 10.f, 2.0e6f}}};
 constexpr float kJoin = 9.0f, kJoinRate = 8e6f;      // us, bytes per us
 constexpr int kMostParts = 32;
+constexpr long long kMostWorkgroups = 1ll << 22;     // of up to 512 threads: a grid has fewer than 2^32
 
 static float form_cost(const FormCost& f, const RaggedArgs& b, int group, int max_q_len, float keys, int e4m3, int parts) {
     const long long tiles_of_rows = min((long long)b.n_seqs * (((long long)max_q_len * group + f.rows - 1) / f.rows),
@@ -1021,6 +1023,7 @@ PagedAttnPlan plan_paged_attention(const RaggedArgs& b, const MaskArgs& mask, in
     }
     const int key_tile = form == 32 ? 32 : 64, tiles = (int)((keys + key_tile - 1) / key_tile);
     if (g_force_parts > 0) parts = min(g_force_parts, max(tiles, 1));
+    parts = (int)max(1ll, min((long long)parts, kMostWorkgroups / (((long long)b.n_tokens * group / form + b.n_seqs) * b.kv_heads)));
     PagedAttnPlan p{form, 1, max(1, (tiles + parts - 1) / parts)};
     p.parts = max(1, (tiles + p.part_tiles - 1) / p.part_tiles);
     return p;

@@ -423,6 +423,60 @@ def test_attention_offsets_beyond_32_bits():
     close(o, want, BF16 * want.abs() + (BF16 + 2.0 ** -12) * mass + 1e-30)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_thousands_of_sequences(e4m3):
+    # more than a lane's worth of sequences for each lane, most of them without a new token
+    r = np.random.RandomState(1)
+    q_len = [int(x) for x in r.choice((0, 0, 1, 3), 5000)]
+    kv_len = [x + int(y) for x, y in zip(q_len, r.randint(0, 20, 5000))]
+    c = Cache(q_len, kv_len, 1, 16, e4m3, pad_tokens=5).fill(1) if not e4m3 else Cache(q_len, kv_len, 1, 16, True, poison=False, pad_tokens=5)
+    k, v = randn(2, c.T, D), randn(3, c.T, D)
+    b.paged_append(c.cfg, c.k, c.v, c.batch, k, v)
+    if not e4m3:
+        for i in (0, 1, 63, 64, 65, 4095, 4096, 4999):
+            for j in range(q_len[i]):
+                at = kv_len[i] - q_len[i] + j
+                assert torch.equal(c.k[c.table[i, at // 16], 0, at % 16], k[c.starts[i] + j])
+    check_attention(c, randn(4, c.T, 2 * D), 2, 1, 0, 0)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("block,window,sink", [(1, 0, 0), (0, 300, 20)])
+def test_lengths_beyond_the_stated_bounds_are_served(block, window, sink, e4m3):
+    c = Cache([1, 70, 9], [3000, 2000, 10], 2, 16, e4m3).fill(1)
+    c.batch = b.ragged_batch(c.q_start, c.kv_len, c.table_dev, c.T, 1, 600)
+    check_attention(c, randn(2, c.T, 8 * D), 8, block, window, sink)
+    c.batch = b.ragged_batch(c.q_start, c.kv_len, c.table_dev, c.T, 0, 0)
+    check_attention(c, randn(2, c.T, 8 * D), 8, block, window, sink)
+
+
+def test_a_kv_len_beyond_the_table_counts_as_the_table():
+    c = Cache([1, 2], [40, 64], 1, 16, extra_entries=0).fill(1)
+    c.kv_len.copy_(ints([40, 1 << 30]))
+    c.kv_len_list = [40, 64]                           # four entries of sixteen
+    check_attention(c, randn(2, c.T, D), 1, 1, 0, 0)
+    c.kv_len.copy_(ints([-5, 64]))
+    c.kv_len_list = [-5, 64]
+    check_attention(c, randn(3, c.T, D), 1, 0, 0, 0)
+
+
+@pytest.mark.parametrize("starts", [[0, 9, 3, 12], [0, 3, 1 << 30, 12], [5, 2, -7, 12], [0, 3, 6, 400]])
+def test_rows_of_no_batch_touch_nothing_outside(starts):
+    """Arrays that are no batch (they do not ascend, or leave the list): whatever rows come out, nothing outside is read or written."""
+    c = Cache([4, 4, 4], [40, 30, 20], 2, 16).fill(1)
+    pool_k, pool_v = c.k.clone(), c.v.clone()
+    c.q_start.copy_(ints(starts))
+    wide = torch.full((c.T + 40, 4 * D), 9.0, dtype=torch.bfloat16, device="cuda")
+    o, q = wide[20:20 + c.T], randn(2, c.T, 4 * D)
+    run_attention(c, q, 4, 1, 0, 0, o=o)
+    assert (wide[:20] == 9.0).all() and (wide[20 + c.T:] == 9.0).all()
+    x, a, w = randn(3, c.T, 64), randn(4, 1, 8, 64), randn(5, 1, 4 * D, 8)
+    ws = torch.empty(b.lora_workspace_bytes(3, c.T, 4, 64, 8), dtype=torch.uint8, device="cuda")
+    b.lora_bf16(x, a, w, None, ints([0, 0, 0]), c.q_start, 4, o, o, ws)
+    assert (wide[:20] == 9.0).all() and (wide[20 + c.T:] == 9.0).all()
+    assert same_bits(c.k, pool_k) and same_bits(c.v, pool_v)
+
+
 # ------------------------------------------------------------------------------------------ adapters
 @pytest.mark.parametrize("q_len,K,N,rank,n,fp32,in_place", [
     ([1], 64, 64, 8, 1, False, False), ([1] * 9, 1536, 4608, 16, 4, False, True), ([5, 0, 40, 1, 130], 320, 448, 24, 3, True, True),

@@ -95,7 +95,8 @@ def test_pool_bytes(lib):
 
 
 BAD_CFG = [dict(struct_size=4), dict(kv_heads=0), dict(page_tokens=8), dict(page_tokens=24), dict(page_tokens=512), dict(n_pages=0), dict(format=2),
-           dict(k_scale=0.0), dict(v_scale=-1.0), dict(k_scale=float("nan")), dict(k_scale=2.0), dict(format=1, v_scale=float("inf"))]
+           dict(k_scale=0.0), dict(v_scale=-1.0), dict(k_scale=float("nan")), dict(k_scale=2.0), dict(format=1, v_scale=float("inf")),
+           dict(format=1, k_scale=1e-39)]
 BAD_BATCH = [dict(struct_size=4), dict(n_seqs=0), dict(n_tokens=-1), dict(max_q_len=-1), dict(max_kv_len=-1), dict(table_stride=0),
              dict(table_stride=1 << 30), dict(q_start=None), dict(kv_len=None), dict(page_table=None), dict(n_tokens=1 << 30)]
 
@@ -181,6 +182,10 @@ def test_lora_workspace_is_checked(lib):
     assert need > 0
     assert lora(lib, lora_cfg(), ws_bytes=need - 1) == SMALL
     assert lora(lib, lora_cfg(), ws=None) == SMALL
+
+
+def test_attention_of_too_many_sequences_is_refused(lib):
+    assert attend(lib, cfg(kv_heads=256), batch(n_seqs=1 << 14), mask(), q_stride=256 * 128, heads=256, o_stride=256 * 128) == INVALID
 
 
 def test_a_batch_without_tokens_is_no_work(lib):
