@@ -2310,7 +2310,7 @@ static const char* lora_wrong(const sdv2_lora_cfg* c) {
     return nullptr;
 }
 
-static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)c->n_tokens * align_up(c->rank, 16) * (parts > 1 ? parts * sizeof(float) : 3 * sizeof(bf16)), 256); }
+static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)parts * c->n_tokens * align_up(c->rank, 16) * sizeof(float), 256); }
 
 size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg) {
     if (const char* why = lora_wrong(cfg)) {
@@ -2355,7 +2355,7 @@ int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* 
     a.rank = cfg->rank;
     a.n_adapters = cfg->n_adapters;
     a.fp32 = cfg->out_fp32;
-    a.u = workspace_dev;
+    a.u = static_cast<float*>(workspace_dev);
     a.u_ranks = (int)align_up(cfg->rank, 16);
     a.parts = parts;
     HIP_TRY(launch_lora(a, cfg->max_q_len, static_cast<hipStream_t>(hip_stream)), "adapter kernels");

@@ -5,8 +5,8 @@
 // are products on 16x16x32 matrix instructions whose fragments come straight from memory (sixteen rows, 64 bytes each), since
 // nothing is used often enough to pay for its way through LDS.
 //   u: computed transposed, ranks as rows and tokens as columns.  A workgroup has 16 or 32 tokens of one sequence and 16 RT ranks; its eight
-//     waves take pieces of 64 of K in turn and add up through LDS.  u is left as two or three bf16 numbers per value that add up to it
-//     (kPieces: as one, its rounding would be the result's largest error).
+//     waves take pieces of 64 of K in turn and add up through LDS.  u is left in 32 bits, and goes to the second product as two or three
+//     bf16 numbers that add up to it (kPieces: as one, its rounding would be the result's largest error).
 //   out: columns of out as rows, tokens as columns, y as the accumulator's start.  The rows of four instructions are interleaved so that a
 //     lane ends up with sixteen columns next to each other of its token.
 #include "ragged.h"
@@ -35,7 +35,7 @@ __device__ __forceinline__ bool locate(const LoraArgs& a, int tile, Tile* t) {
 
 constexpr int kDownWaves = 8;
 // bf16 numbers that one of u goes to the second product as: each takes off eight bits, and an output of 32 bits shows the 17th
-// (four frames of rank 64 against 64 bits: two pieces 1.9e-6 of the output, three 3e-7, which is the sum's own).
+// (four frames of rank 64 against 64 bits: two pieces 1.9e-6 of the output, three 1.2e-7, which is the sum's own).
 template <typename T>
 constexpr int kPieces = sizeof(T) == 4 ? 3 : 2;
 
@@ -99,25 +99,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
         for (int k = 1; k < kDownWaves; ++k) u += parts[k][b][lane];
         const int rank = rank0 + 16 * (b / NT) + 4 * lk, token = 16 * (b % NT) + l15;      // four ranks of one token
         if (token >= t.count || rank >= a.u_ranks) continue;
-        if (NT == 1) {                       // few tokens: the vector unit's form, 32 bits
 #pragma unroll
-            for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
-            *reinterpret_cast<f32x4*>(static_cast<float*>(a.u) + ((long long)part * a.n_tokens + t.first + token) * a.u_ranks + rank) = u;
-            continue;
-        }
-        bf16* const to = static_cast<bf16*>(a.u) + (long long)(t.first + token) * a.pieces * a.u_ranks + rank;
-        f32x4 rest;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) rest[e] = rank < a.rank ? u[e] * scale : 0.0f;
-        for (int p = 0; p < a.pieces; ++p) {
-            bf16x4 piece;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                piece[e] = (bf16)rest[e];
-                rest[e] -= (float)piece[e];
-            }
-            *reinterpret_cast<bf16x4*>(to + (long long)p * a.u_ranks) = piece;
-        }
+        for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
+        *reinterpret_cast<f32x4*>(a.u + ((long long)part * a.n_tokens + t.first + token) * a.u_ranks + rank) = u;
     }
 }
 
@@ -164,71 +148,91 @@ struct Sixteen<bf16> {
     }
 };
 
-// KS: steps of 32 ranks.  A wave has NB blocks of 64 columns and the tile's tokens, sixteen at a time.
-template <typename T, int KS, int NB, int TOKENS>
+// KS: steps of 32 ranks.  A wave has a block of 64 columns, whose rows of B it holds, and the tile's tokens, sixteen at a time: the next
+// sixteen's y and u are on their way under this one's products.
+template <typename T, int KS, int TOKENS>
 __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned groups) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l15 = lane & 15, lk = lane >> 4;
     const unsigned tile = blockIdx.x / groups;
-    const int block0 = ((int)(blockIdx.x - tile * groups) * 4 + wave) * NB, blocks = a.N >> 6;
-    if (block0 >= blocks) return;
+    const int block = (int)(blockIdx.x - tile * groups) * 4 + wave;
+    if (block >= (a.N >> 6)) return;
     Tile t;
     if (!locate<TOKENS>(a, (int)tile, &t)) return;
-    const T* const y = static_cast<const T*>(a.y);
-    T* const out = static_cast<T*>(a.out);
-    constexpr int NG = TOKENS / 16;                           // sixteens of tokens: their loads are in flight together
-    Sixteen<T> v[NG][NB];
+    const T* const y = static_cast<const T*>(a.y) + block * 64;
+    T* const out = static_cast<T*>(a.out) + block * 64;
+    auto row_of = [&](int g) { return (long long)t.first + min(16 * g + l15, t.count - 1); };
+    constexpr int NG = TOKENS / 16, NP = kPieces<T>;
+    if (t.adapter < 0) {
+        if (a.y == a.out) return;
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-            if (16 * g + l15 < t.count)
-                v[g][b].load(y + (long long)(t.first + 16 * g + l15) * a.y_stride + min(block0 + b, blocks - 1) * 64, lk);
-    bf16x8 w[NB][4][KS], u[kPieces<T>][KS];
-    if (t.adapter >= 0) {
-        const bf16x8 none = {};
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                const bf16* const p = a.b + ((long long)t.adapter * a.N + min(block0 + b, blocks - 1) * 64 + Sixteen<T>::column(m, l15)) * a.rank;
-#pragma unroll
-                for (int k = 0; k < KS; ++k) w[b][m][k] = 32 * k + 8 * lk < a.rank ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
-            }
-    } else if (a.y == a.out) {
+        for (int g = 0; g < NG; ++g) {
+            if (16 * g + l15 >= t.count) continue;
+            Sixteen<T> v;
+            v.load(y + row_of(g) * a.y_stride, lk);
+            const f32x4 same[4] = {v.four(0), v.four(1), v.four(2), v.four(3)};
+            Sixteen<T>::store(out + row_of(g) * a.out_stride, lk, same);
+        }
         return;
     }
+    struct Group {
+        Sixteen<T> v;
+        f32x4 u[KS][2];
+    };
+    // ranks past the end, of which the products must see zeros on both sides (infinities and NaN), are copies of the last until then
+    const bool cut = (a.rank & 31) != 0;
+    auto fetch = [&](int g) {
+        Group x;
+        x.v.load(y + row_of(g) * a.y_stride, lk);
+        const float* const p = a.u + row_of(g) * a.u_ranks;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) x.u[k][h] = *reinterpret_cast<const f32x4*>(p + min(32 * k + 8 * lk, a.u_ranks - 8) + 4 * h);
+        return x;
+    };
+    Group next = fetch(0);
+    bf16x8 w[4][KS];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        const bf16* const p = a.b + ((long long)t.adapter * a.N + block * 64 + Sixteen<T>::column(m, l15)) * a.rank;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) w[m][k] = *reinterpret_cast<const bf16x8*>(p + min(32 * k + 8 * lk, a.rank - 8));
+    }
     __builtin_amdgcn_sched_barrier(0);
+    const bf16x8 none = {};
+    if (cut) {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) w[m][KS - 1] = 32 * (KS - 1) + 8 * lk < a.rank ? w[m][KS - 1] : none;
+    }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-        const bool live = 16 * g + l15 < t.count;
-        const long long row = t.first + min(16 * g + l15, t.count - 1);
-        f32x4 acc[NB][4];
+        if (16 * g >= t.count) break;
+        Group now = next;
+        if (g + 1 < NG && 16 * (g + 1) < t.count) next = fetch(g + 1);
+        __builtin_amdgcn_sched_barrier(0);
+        if (cut && 32 * (KS - 1) + 8 * lk >= a.rank) now.u[KS - 1][0] = now.u[KS - 1][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        f32x4 acc[4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int m = 0; m < 4; ++m) acc[m] = now.v.four(m);
 #pragma unroll
-            for (int m = 0; m < 4; ++m) acc[b][m] = v[g][b].four(m);
-        if (t.adapter >= 0) {
-            const bf16x8 none = {};
+        for (int k = 0; k < KS; ++k) {
+            bf16x8 piece[NP];
 #pragma unroll
-            for (int h = 0; h < kPieces<T>; ++h)
+            for (int e = 0; e < 8; ++e) {
+                float rest = now.u[k][e >> 2][e & 3];
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    const bf16* const p = static_cast<const bf16*>(a.u) + ((long long)(t.first + min(16 * g + l15, t.count - 1)) * kPieces<T> + h) * a.u_ranks;
-                    u[h][k] = 32 * k + 8 * lk < a.u_ranks ? *reinterpret_cast<const bf16x8*>(p + 32 * k + 8 * lk) : none;
+                for (int h = 0; h < NP; ++h) {
+                    piece[h][e] = (bf16)rest;
+                    rest -= (float)piece[h][e];
                 }
+            }
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
+            for (int h = NP - 1; h >= 0; --h)
 #pragma unroll
-                for (int h = kPieces<T> - 1; h >= 0; --h)
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-#pragma unroll
-                        for (int m = 0; m < 4; ++m) acc[b][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[b][m][k], u[h][k], acc[b][m], 0, 0, 0);
+                for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[m][k], piece[h], acc[m], 0, 0, 0);
         }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-            if (live && block0 + b < blocks) Sixteen<T>::store(out + row * a.out_stride + (block0 + b) * 64, lk, acc[b]);
+        if (16 * g + l15 < t.count) Sixteen<T>::store(out + row_of(g) * a.out_stride, lk, acc);
     }
 }
 
@@ -274,7 +278,7 @@ __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned g
                 const int r = r0 + (lane & (16 * CH - 1));
                 float u = 0.0f;
                 for (int p = 0; p < a.parts; ++p)
-                    u += r < a.u_ranks ? static_cast<const float*>(a.u)[((long long)p * a.n_tokens + row) * a.u_ranks + r] : 0.0f;
+                    u += r < a.u_ranks ? a.u[((long long)p * a.n_tokens + row) * a.u_ranks + r] : 0.0f;
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
 #pragma unroll
@@ -298,14 +302,14 @@ void launch_up(const LoraArgs& a, bool few, hipStream_t s) {
         else hipLaunchKernelGGL((lora_up_few_kernel<T, 4>), grid, dim3(256), 0, s, a, groups);
         return;
     }
-    constexpr int NB = 1, TOKENS = 32;
-    const unsigned groups = (unsigned)(a.N / 64 + 4 * NB - 1) / (4 * NB);
+    constexpr int TOKENS = 32;
+    const unsigned groups = (unsigned)(a.N / 64 + 3) / 4;
     const dim3 grid(groups * (unsigned)(a.n_tokens / TOKENS + a.n_seqs));
     switch ((a.u_ranks + 31) / 32) {
-        case 1: hipLaunchKernelGGL((lora_up_kernel<T, 1, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
-        case 2: hipLaunchKernelGGL((lora_up_kernel<T, 2, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
-        case 3: hipLaunchKernelGGL((lora_up_kernel<T, 3, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
-        default: hipLaunchKernelGGL((lora_up_kernel<T, 4, NB, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
+        case 1: hipLaunchKernelGGL((lora_up_kernel<T, 1, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
+        case 2: hipLaunchKernelGGL((lora_up_kernel<T, 2, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
+        case 3: hipLaunchKernelGGL((lora_up_kernel<T, 3, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
+        default: hipLaunchKernelGGL((lora_up_kernel<T, 4, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
     }
 }
 template <int NT, int RT>
@@ -322,9 +326,7 @@ int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
     return max(1, min(min(kUnits / workgroups, K / 1024), 4));
 }
 
-hipError_t launch_lora(const LoraArgs& args, int max_q_len, hipStream_t s) {
-    LoraArgs a = args;
-    a.pieces = a.fp32 ? kPieces<float> : kPieces<bf16>;
+hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
     const bool few = max_q_len <= 16;
     if (few) launch_down<1, 1>(a, s);
     else if (a.n_tokens < 4096 || a.u_ranks < 64) launch_down<2, 2>(a, s);

@@ -149,10 +149,9 @@ struct LoraArgs {
     void* out;
     long long x_stride, y_stride, out_stride;
     int n_seqs, n_tokens, K, N, rank, n_adapters, fp32;
-    void* u;                          // scale x A^T: [n_tokens][pieces][u_ranks] bf16; few tokens, K in parts: [parts][n_tokens][u_ranks] fp32
+    float* u;                         // scale x A^T, K in parts: [parts][n_tokens][u_ranks]
     int u_ranks;                      // rank rounded up to 16
     int parts;
-    int pieces;                       // set by the launcher
 };
 // parts of K: n_seqs, n_tokens, max_q_len, K, rank
 int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank);
