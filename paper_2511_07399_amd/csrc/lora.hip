@@ -189,6 +189,15 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
         for (int k = 0; k < KS; ++k)
 #pragma unroll
             for (int h = 0; h < 2; ++h) x.u[k][h] = *reinterpret_cast<const f32x4*>(p + min(32 * k + 8 * lk, a.u_ranks - 8) + 4 * h);
+        if (NG == 1) {
+            for (int part = 1; part < a.parts; ++part) {
+                const float* const o = p + (long long)part * a.n_tokens * a.u_ranks;
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) x.u[k][h] += *reinterpret_cast<const f32x4*>(o + min(32 * k + 8 * lk, a.u_ranks - 8) + 4 * h);
+            }
+        }
         return x;
     };
     Group next = fetch(0);
@@ -236,73 +245,81 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
     }
 }
 
-// Few tokens of a sequence: on the vector unit, where a tile of sixteen tokens would mostly be empty and its accumulators cost the places
-// of other waves.  A lane has two columns, 16 CH ranks of which it holds at once; u, summed over the parts of K, goes round by
-// readlane.  64 tokens of rank 16 over 15 360 columns: 12.5 us on the matrix instructions, 7.8 with one part of K, so.
-template <typename T, int CH>
+// One token of a sequence: on the vector unit, where a tile would be empty but for one of sixteen tokens.  B's rows lie one behind the
+// other, so lanes next to each other read pieces of eight ranks next to each other: P lanes have a column (P the power of two from the
+// pieces of a row on), 64 / P columns a load, and add up by moves within the row of lanes; of the P loads that cover 64 columns a lane
+// keeps the sum of one, its own.  B's bytes bound it: 64 tokens of 16 adapters beside 5120 x 15 360, both launches, rank 16 15.2 us, 64
+// 31.2, 128 48.4 (by tiles 18.5, -, 59.5; a lane with columns of its own, 16 bytes of 64 lines a load, 15.0 and 48.6 at ranks 16 and 64).
+template <int P>
+__device__ __forceinline__ float piece_sum(float v) {
+    if (P >= 2) v += dpp_f<0xB1>(v);         // quad_perm [1, 0, 3, 2]
+    if (P >= 4) v += dpp_f<0x4E>(v);         // quad_perm [2, 3, 0, 1]
+    if (P >= 8) v += dpp_f<0x141>(v);        // row_half_mirror
+    if (P >= 16) v += dpp_f<0x140>(v);       // row_mirror
+    return v;
+}
+template <typename T, int P>
 __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned groups) {
+    constexpr int kBlocks = P >= 4 ? 1 : 4 / P;                // blocks of 64 columns of a wave: four loads or more at once
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int piece = lane & (P - 1), c = lane / P;
     const unsigned tile = blockIdx.x / groups;
-    const int n = ((int)(blockIdx.x - tile * groups) * 4 + wave) * 128 + 2 * lane;
+    const int block0 = ((int)(blockIdx.x - tile * groups) * 4 + wave) * kBlocks, blocks = a.N >> 6;
+    if (block0 >= blocks) return;
     Tile t;
     if (!locate<16>(a, (int)tile, &t)) return;
-    typedef T T2 __attribute__((ext_vector_type(2)));
-    const bool live = n < a.N;
-    const int at = min(n, a.N - 2);
     const T* const y = static_cast<const T*>(a.y);
     T* const out = static_cast<T*>(a.out);
     const bool adapted = t.adapter >= 0;
     if (!adapted && a.y == a.out) return;
-    const bf16* const rows = a.b + ((long long)max(t.adapter, 0) * a.N + at) * a.rank;
-    bf16x8 w[2][CH][2];
-    auto fetch = [&](int r0) {
+    // the lane's column of a block, and its piece of the rows of the columns that it adds up for others
+    const int own = piece * (64 / P) + c;
+    const bool there = 8 * piece < a.rank;                     // (a row of pieces that is no power of two)
+    bf16x8 w[kBlocks][P];
+    if (adapted) {
+        const bf16* const p = a.b + (long long)t.adapter * a.N * a.rank + min(8 * piece, a.rank - 8);
 #pragma unroll
-        for (int c = 0; c < CH; ++c)
+        for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = r0 + 16 * c + 8 * h;
-                    w[i][c][h] = *reinterpret_cast<const bf16x8*>(rows + (long long)i * a.rank + min(r, a.rank - 8));       // past the end: times u = 0
-                }
-    };
-    const bool once = a.rank <= 16 * CH;
-    if (adapted && once) fetch(0);
+            for (int g = 0; g < P; ++g)
+                w[b][g] = *reinterpret_cast<const bf16x8*>(p + (long long)(min(block0 + b, blocks - 1) * 64 + g * (64 / P) + c) * a.rank);
+    }
     for (int i = 0; i < t.count; ++i) {
         const long long row = t.first + i;
-        const T2 own = *reinterpret_cast<const T2*>(y + row * a.y_stride + at);
-        float x0 = (float)own[0], x1 = (float)own[1];
-        if (adapted)
-            for (int r0 = 0; r0 < a.rank; r0 += 16 * CH) {
-                if (!once) fetch(r0);
-                const int r = r0 + (lane & (16 * CH - 1));
-                float u = 0.0f;
-                for (int p = 0; p < a.parts; ++p)
-                    u += r < a.u_ranks ? a.u[((long long)p * a.n_tokens + row) * a.u_ranks + r] : 0.0f;
+        T v[kBlocks];
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
+        for (int b = 0; b < kBlocks; ++b) v[b] = y[row * a.y_stride + min(block0 + b, blocks - 1) * 64 + own];
+        float x[kBlocks];
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float ue = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(u), 16 * c + e));
-                        x0 = fmaf(ue, (float)w[0][c][e >> 3][e & 7], x0);
-                        x1 = fmaf(ue, (float)w[1][c][e >> 3][e & 7], x1);
-                    }
-            }
-        if (live) *reinterpret_cast<T2*>(out + row * a.out_stride + n) = T2{(T)x0, (T)x1};
+        for (int b = 0; b < kBlocks; ++b) x[b] = 0.0f;
+        if (adapted) {
+            f32x4 u[2] = {};
+            if (there)
+                for (int p = 0; p < a.parts; ++p) {
+                    const f32x4* const up = reinterpret_cast<const f32x4*>(a.u + ((long long)p * a.n_tokens + row) * a.u_ranks + 8 * piece);
+                    u[0] += up[0];
+                    u[1] += up[1];
+                }
+#pragma unroll
+            for (int b = 0; b < kBlocks; ++b)
+#pragma unroll
+                for (int g = 0; g < P; ++g) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum = fmaf(u[e >> 2][e & 3], (float)w[b][g][e], sum);
+                    sum = there ? sum : 0.0f;
+                    sum = piece_sum<P>(sum);
+                    x[b] = piece == g ? sum : x[b];
+                }
+        }
+#pragma unroll
+        for (int b = 0; b < kBlocks; ++b)
+            if (block0 + b < blocks) out[row * a.out_stride + (block0 + b) * 64 + own] = adapted ? (T)((float)v[b] + x[b]) : v[b];
     }
 }
 
-template <typename T>
-void launch_up(const LoraArgs& a, bool few, hipStream_t s) {
-    if (few) {
-        const unsigned groups = (unsigned)(a.N + 511) / 512;
-        const dim3 grid(groups * (unsigned)(a.n_tokens / 16 + a.n_seqs));
-        if (a.rank <= 16) hipLaunchKernelGGL((lora_up_few_kernel<T, 1>), grid, dim3(256), 0, s, a, groups);
-        else if (a.rank <= 32) hipLaunchKernelGGL((lora_up_few_kernel<T, 2>), grid, dim3(256), 0, s, a, groups);
-        else hipLaunchKernelGGL((lora_up_few_kernel<T, 4>), grid, dim3(256), 0, s, a, groups);
-        return;
-    }
-    constexpr int TOKENS = 32;
+template <typename T, int TOKENS>
+void launch_up_tiles(const LoraArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)(a.N / 64 + 3) / 4;
     const dim3 grid(groups * (unsigned)(a.n_tokens / TOKENS + a.n_seqs));
     switch ((a.u_ranks + 31) / 32) {
@@ -311,6 +328,23 @@ void launch_up(const LoraArgs& a, bool few, hipStream_t s) {
         case 3: hipLaunchKernelGGL((lora_up_kernel<T, 3, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
         default: hipLaunchKernelGGL((lora_up_kernel<T, 4, TOKENS>), grid, dim3(256), 0, s, a, groups); break;
     }
+}
+template <typename T>
+void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
+    if (max_q_len == 1) {
+        auto go = [&](auto kernel, int blocks) {
+            const unsigned groups = (unsigned)(a.N / 64 + 4 * blocks - 1) / (4 * blocks);
+            hipLaunchKernelGGL(kernel, dim3(groups * (unsigned)(a.n_tokens / 16 + a.n_seqs)), dim3(256), 0, s, a, groups);
+        };
+        if (a.rank <= 8) go(lora_up_few_kernel<T, 1>, 4);
+        else if (a.rank <= 16) go(lora_up_few_kernel<T, 2>, 2);
+        else if (a.rank <= 32) go(lora_up_few_kernel<T, 4>, 1);
+        else if (a.rank <= 64) go(lora_up_few_kernel<T, 8>, 1);
+        else go(lora_up_few_kernel<T, 16>, 1);
+        return;
+    }
+    if (max_q_len <= 16) launch_up_tiles<T, 16>(a, s);
+    else launch_up_tiles<T, 32>(a, s);
 }
 template <int NT, int RT>
 void launch_down(const LoraArgs& a, hipStream_t s) {
@@ -333,8 +367,8 @@ hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
     else launch_down<2, 4>(a, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.fp32) launch_up<float>(a, few, s);
-    else launch_up<bf16>(a, few, s);
+    if (a.fp32) launch_up<float>(a, max_q_len, s);
+    else launch_up<bf16>(a, max_q_len, s);
     return hipGetLastError();
 }
 

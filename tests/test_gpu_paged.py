@@ -291,6 +291,7 @@ SHAPES = [
     ([200], [3000], 6, 3, 16),
     ([5, 20], [3, 20], 3, 3, 32),                       # more new tokens than tokens
     ([4, 2, 1], [6000, 100, 9000], 16, 2, 64),
+    ([3, 30], [400, 90], 300, 1, 16),                   # more heads in a group than rows in any workgroup
 ]
 
 
@@ -319,7 +320,7 @@ FORMS = [(32, 1), (32, 7), (128, 1), (128, 4), (256, 1), (256, 3)]
 
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("block,window,sink", [(1, 0, 0), (24, 0, 0), (1, 100, 30)])
-@pytest.mark.parametrize("shape", [2, 4, 5, 6, 7, 8, 9])
+@pytest.mark.parametrize("shape", [2, 4, 5, 6, 7, 8, 9, 10])
 @pytest.mark.parametrize("form", FORMS, indirect=True)
 def test_every_form_of_attention(form, shape, block, window, sink, e4m3):
     test_attention(shape, block, window, sink, e4m3)
@@ -362,12 +363,9 @@ def test_attention_does_not_see_pages_that_are_gone(q_len, e4m3):
     assert (run_attention(c, randn(6, c.T, 4 * D), 4, 1, 0, 0)[:c.starts[-1]] == 0).all()
 
 
-@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("e4m3,bad", [(False, float("nan")), (False, float("inf")), (False, -float("inf")), (True, float("nan"))])      # e4m3 has no infinity
 @pytest.mark.parametrize("q_len,kv_len", [(6, 6), (40, 100), (300, 300), (130, 1000)])
 def test_what_a_row_does_not_see_does_not_reach_it(q_len, kv_len, e4m3, bad):
-    if e4m3 and not math.isnan(bad):
-        pytest.skip("e4m3 has no infinity")
     c = Cache([q_len, 2], [kv_len, 9], 2, 16, e4m3).fill(8)
     q = randn(9, c.T, 4 * D)
     clean, _ = attention_64(c, q, 4, 1, 0, 0)
@@ -421,6 +419,17 @@ def test_attention_offsets_beyond_32_bits():
             small.k[small.table[i, e]], small.v[small.table[i, e]] = c.k[c.table[i, e]], c.v[c.table[i, e]]
     want, mass = attention_64(small, q, heads, 1, 0, 0)
     close(o, want, BF16 * want.abs() + (BF16 + 2.0 ** -12) * mass + 1e-30)
+
+
+def test_a_batch_without_tokens_launches_nothing():
+    c = Cache([0, 0], [40, 0], 2, 16)
+    none = torch.empty(0, 2 * D, dtype=torch.bfloat16, device="cuda")
+    b.paged_append(c.cfg, c.k, c.v, c.batch, none, none, b.rope_cfg(1), torch.empty(0, 1, dtype=torch.int32, device="cuda"), None, none, none.clone())
+    b.paged_attention(c.cfg, c.k, c.v, c.batch, b.attn_mask(1), none, none.clone())
+    b.qk_norm_rope(b.rope_cfg(0), None, none, none.clone())
+    b.lora_bf16(none, randn(1, 1, 8, 2 * D), randn(2, 1, 64, 8), None, ints([0, 0]), c.q_start, 0, torch.empty(0, 64, device="cuda"),
+                torch.empty(0, 64, device="cuda"), None)
+    assert c.k.isnan().all() and c.v.isnan().all()
 
 
 @pytest.mark.parametrize("e4m3", [False, True])
@@ -481,7 +490,8 @@ def test_rows_of_no_batch_touch_nothing_outside(starts):
 @pytest.mark.parametrize("q_len,K,N,rank,n,fp32,in_place", [
     ([1], 64, 64, 8, 1, False, False), ([1] * 9, 1536, 4608, 16, 4, False, True), ([5, 0, 40, 1, 130], 320, 448, 24, 3, True, True),
     ([300, 77], 512, 128, 64, 2, True, False), ([64, 200, 1], 128, 1024, 128, 3, False, False), ([3] * 100, 256, 192, 32, 7, False, True),
-    ([1, 2], 5120, 640, 16, 2, True, False)])
+    ([1, 2], 5120, 640, 16, 2, True, False), ([1] * 5, 1024, 320, 128, 3, True, False), ([1, 7, 16], 640, 192, 40, 2, False, False),
+    ([9] * 300, 128, 64, 64, 5, True, True), ([2], 704, 2112, 72, 1, False, True)])
 def test_lora(q_len, K, N, rank, n, fp32, in_place):
     starts = [0] + list(np.cumsum(q_len))
     T = int(starts[-1]) + 2
@@ -493,7 +503,7 @@ def test_lora(q_len, K, N, rank, n, fp32, in_place):
     out = y if in_place else torch.full((T, N), 4.0, dtype=y.dtype, device="cuda")
     y0 = y.clone()
     need = b.lora_workspace_bytes(len(q_len), T, max(q_len), K, rank)
-    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None
     b.lora_bf16(x, a, w, scale, ints(ids), ints(starts), max(q_len), y, out, ws)
     want = y0.double().cpu()
     err = torch.zeros_like(want)
