@@ -2310,7 +2310,12 @@ static const char* lora_wrong(const sdv2_lora_cfg* c) {
     return nullptr;
 }
 
-static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) { return align_up((size_t)parts * c->n_tokens * align_up(c->rank, 16) * sizeof(float), 256); }
+// sixteens of tokens of one sequence each, as the kernels number them; none where every sequence has one token at most
+static int lora_slots(const sdv2_lora_cfg* c) { return c->n_tokens > 0 && c->max_q_len > 1 ? c->n_tokens / 16 + c->n_seqs : 0; }
+static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) {
+    const size_t rows = lora_slots(c) ? (size_t)lora_slots(c) * 16 : c->n_tokens;
+    return align_up(parts * rows * align_up(c->rank, 16) * sizeof(float), 256);
+}
 
 size_t sdv2_lora_workspace_bytes(const sdv2_lora_cfg* cfg) {
     if (const char* why = lora_wrong(cfg)) {
@@ -2358,6 +2363,7 @@ int32_t sdv2_lora_bf16(const sdv2_lora_cfg* cfg, const void* a_dev, const void* 
     a.u = static_cast<float*>(workspace_dev);
     a.u_ranks = (int)align_up(cfg->rank, 16);
     a.parts = parts;
+    a.slots = lora_slots(cfg);
     HIP_TRY(launch_lora(a, cfg->max_q_len, static_cast<hipStream_t>(hip_stream)), "adapter kernels");
     return SDV2_OK;
 }

@@ -19,6 +19,7 @@ namespace {
 // sequence s start at floor(q_start[s] / tokens) + s.
 struct Tile {
     int first, count, adapter;        // first row of the batch, rows (<= tokens), adapter or -1
+    int slot;                         // of u: sixteens of tokens, numbered as tiles of sixteen
 };
 template <int TOKENS>
 __device__ __forceinline__ bool locate(const LoraArgs& a, int tile, Tile* t) {
@@ -29,8 +30,18 @@ __device__ __forceinline__ bool locate(const LoraArgs& a, int tile, Tile* t) {
     if (at < 0 || at >= n) return false;
     t->first = q0 + at;
     t->count = min(TOKENS, n - at);
+    t->slot = q0 / 16 + s.index + at / 16;
     t->adapter = (unsigned)id < (unsigned)a.n_adapters ? id : -1;
     return true;
+}
+
+// u between the launches: by sixteens of tokens, and of those by fours of ranks, [slot][rank / 4][16 tokens][4], so that the sixteen
+// lanes of a fragment's rows have 256 bytes next to each other; a row for a token where the second product has one token at a time.
+__device__ __forceinline__ float* u_at(const LoraArgs& a, int part, int slot, int rank, int token) {
+    return a.u + ((long long)part * a.slots + slot) * 16 * a.u_ranks + rank * 16 + token * 4;
+}
+__device__ __forceinline__ float* u_row(const LoraArgs& a, int part, int row, int rank) {
+    return a.u + ((long long)part * a.n_tokens + row) * a.u_ranks + rank;
 }
 
 constexpr int kDownWaves = 8;
@@ -39,9 +50,9 @@ constexpr int kDownWaves = 8;
 template <typename T>
 constexpr int kPieces = sizeof(T) == 4 ? 3 : 2;
 
-template <int NT, int RT>
 __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, unsigned groups) {
-    __shared__ f32x4 parts[kDownWaves][RT * NT][64];
+    __shared__ f32x4 parts[kDownWaves][1][64];
+    constexpr int NT = 1, RT = 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l15 = lane & 15, lk = lane >> 4;
     const unsigned rest = blockIdx.x / a.parts, part = blockIdx.x - rest * a.parts, tile = rest / groups;
@@ -101,118 +112,188 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
         if (token >= t.count || rank >= a.u_ranks) continue;
 #pragma unroll
         for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
-        *reinterpret_cast<f32x4*>(a.u + ((long long)part * a.n_tokens + t.first + token) * a.u_ranks + rank) = u;
+        *reinterpret_cast<f32x4*>(a.slots != 0 ? u_at(a, part, t.slot + (b % NT), rank, l15) : u_row(a, part, t.first + token, rank)) = u;
     }
 }
 
-// A lane's sixteen columns of a block of 64 of y or out: pieces of 16 bytes such that the four lanes of a token have 64 bytes next to each
-// other in each.  Which column of the block instruction m's row r is, goes by that: column(m, r).
-template <typename T>
-struct Sixteen;
-template <>
-struct Sixteen<float> {
-    f32x4 x[4];
-    static __device__ __forceinline__ int column(int m, int r) { return 16 * m + r; }
-    __device__ __forceinline__ void load(const float* p, int lk) {
+// The same for 32 tokens of a longer sequence and up to 64 ranks (16 RT), through LDS: a row's line of 128 bytes goes to eight lanes next
+// to each other, where a fragment's lanes next to each other have different rows, each an access of the cache by itself.  Each wave has
+// a stage of its own, and two pieces of 64 of K on their way to its registers.
+template <int RT>
+__global__ __launch_bounds__(256) void lora_down_tile_kernel(LoraArgs a, unsigned groups) {
+    constexpr int kWaves = 4, kRows = 16 * RT + 32, kLoads = kRows / 8;
+    __shared__ bf16x8 stage[kWaves][kRows * 8];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l15 = lane & 15, lk = lane >> 4;
+    const unsigned tile = blockIdx.x / groups;
+    Tile t;
+    if (!locate<32>(a, (int)tile, &t) || t.adapter < 0) return;
+    const int rank0 = (int)(blockIdx.x - tile * groups) * (16 * RT);
+    const float scale = a.scale != nullptr ? a.scale[t.adapter] : 1.0f;
+
+    // rows of the stage: the ranks, then the tokens; sixteen bytes c of row r lie at place c ^ (r / 2 & 7)
+    const bf16* from[kLoads];
+    int to[kLoads];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) x[m] = *reinterpret_cast<const f32x4*>(p + 16 * m + 4 * lk);
+    for (int i = 0; i < kLoads; ++i) {
+        const int r = 8 * i + (lane >> 3), c = lane & 7;
+        from[i] = 8 * i < 16 * RT ? a.a + ((long long)t.adapter * a.rank + min(rank0 + r, a.rank - 1)) * a.K + 8 * c
+                                  : a.x + (long long)(t.first + min(r - 16 * RT, t.count - 1)) * a.x_stride + 8 * c;
+        to[i] = r * 8 + (c ^ (r >> 1 & 7));
     }
-    __device__ __forceinline__ f32x4 four(int m) const { return x[m]; }
-    static __device__ __forceinline__ void store(float* p, int lk, const f32x4 (&v)[4]) {
+    bf16x8* const mine = stage[wave];
+    f32x4 acc[RT][2];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) *reinterpret_cast<f32x4*>(p + 16 * m + 4 * lk) = v[m];
-    }
-};
-template <>
-struct Sixteen<bf16> {
-    bf16x8 x[2];
-    static __device__ __forceinline__ int column(int m, int r) { return 32 * (m >> 1) + 8 * (r >> 2) + 4 * (m & 1) + (r & 3); }
-    __device__ __forceinline__ void load(const bf16* p, int lk) {
+    for (int i = 0; i < RT; ++i) acc[i][0] = acc[i][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const int pieces = a.K >> 6;
+    struct Piece {
+        bf16x8 v[kLoads];
+    };
+    auto fetch = [&](int p) {
+        Piece x;
+        const int at = min(p, pieces - 1) * 64;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) x[h] = *reinterpret_cast<const bf16x8*>(p + 32 * h + 8 * lk);
-    }
-    __device__ __forceinline__ f32x4 four(int m) const {
-        f32x4 r;
+        for (int i = 0; i < kLoads; ++i) x.v[i] = *reinterpret_cast<const bf16x8*>(from[i] + at);
+        return x;
+    };
+    auto multiply = [&](const Piece& x) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r[e] = (float)x[m >> 1][4 * (m & 1) + e];
-        return r;
-    }
-    static __device__ __forceinline__ void store(bf16* p, int lk, const f32x4 (&v)[4]) {
+        for (int i = 0; i < kLoads; ++i) mine[to[i]] = x.v[i];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");         // (other lanes' writes)
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            bf16x8 o;
+            bf16x8 w[RT], v[2];
+            auto row = [&](int r) { return mine[(r + l15) * 8 + ((4 * h + lk) ^ (l15 >> 1))]; };
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = (bf16)v[2 * h + (e >> 2)][e & 3];
-            *reinterpret_cast<bf16x8*>(p + 32 * h + 8 * lk) = o;
+            for (int i = 0; i < RT; ++i) w[i] = row(16 * i);
+#pragma unroll
+            for (int j = 0; j < 2; ++j) v[j] = row(16 * RT + 16 * j);
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[i], v[j], acc[i][j], 0, 0, 0);
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    Piece first = fetch(wave), second = fetch(wave + kWaves);
+    for (int p = wave; p < pieces; p += 2 * kWaves) {
+        multiply(first);
+        first = fetch(p + 2 * kWaves);
+        __builtin_amdgcn_sched_barrier(0);
+        if (p + kWaves >= pieces) break;
+        multiply(second);
+        second = fetch(p + 3 * kWaves);
+        __builtin_amdgcn_sched_barrier(0);
     }
-};
+    __syncthreads();
+    f32x4* const parts = reinterpret_cast<f32x4*>(stage);              // [wave][block][lane]
+    static_assert(kWaves * RT * 2 * 64 <= kWaves * kRows * 8, "the sums fit the stage");
+#pragma unroll
+    for (int i = 0; i < RT; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) parts[(wave * RT * 2 + i * 2 + j) * 64 + lane] = acc[i][j];
+    __syncthreads();
+    for (int b = wave; b < RT * 2; b += kWaves) {
+        f32x4 u = parts[b * 64 + lane];
+#pragma unroll
+        for (int k = 1; k < kWaves; ++k) u += parts[(k * RT * 2 + b) * 64 + lane];
+        const int rank = rank0 + 16 * (b >> 1) + 4 * lk;               // four ranks of one token
+        if (16 * (b & 1) + l15 >= t.count || rank >= a.u_ranks) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
+        *reinterpret_cast<f32x4*>(u_at(a, 0, t.slot + (b & 1), rank, l15)) = u;
+    }
+}
 
-// KS: steps of 32 ranks.  A wave has a block of 64 columns, whose rows of B it holds, and the tile's tokens, sixteen at a time: the next
-// sixteen's y and u are on their way under this one's products.
+// KS: steps of 32 ranks.  A wave has a block of 64 columns and the tile's tokens, sixteen at a time: the next sixteen's y and u are on
+// their way under this one's products.  Tokens are the rows of the result and lane l15 has columns 4 l15 .. + 3 (of four instructions),
+// so a token's y and out are sixteen lanes next to each other; B's rows, of one piece of memory, are turned into fragments through LDS.
 template <typename T, int KS, int TOKENS>
 __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned groups) {
+    typedef T four __attribute__((ext_vector_type(4)));
+    __shared__ bf16x8 stage[4][64 * (4 * KS + 1)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l15 = lane & 15, lk = lane >> 4;
     const unsigned tile = blockIdx.x / groups;
     const int block = (int)(blockIdx.x - tile * groups) * 4 + wave;
-    if (block >= (a.N >> 6)) return;
+    if (block >= (a.N >> 6)) return;                           // (no barrier follows: a wave's stage is its own)
     Tile t;
     if (!locate<TOKENS>(a, (int)tile, &t)) return;
-    const T* const y = static_cast<const T*>(a.y) + block * 64;
-    T* const out = static_cast<T*>(a.out) + block * 64;
-    auto row_of = [&](int g) { return (long long)t.first + min(16 * g + l15, t.count - 1); };
+    const T* const y = static_cast<const T*>(a.y) + block * 64 + 4 * l15;
+    T* const out = static_cast<T*>(a.out) + block * 64 + 4 * l15;
     constexpr int NG = TOKENS / 16, NP = kPieces<T>;
+    auto token = [&](int g, int e) { return 16 * g + 4 * lk + e; };
+    auto load = [&](int g, int e) { return *reinterpret_cast<const four*>(y + (long long)(t.first + min(token(g, e), t.count - 1)) * a.y_stride); };
+    auto store = [&](int g, int e, four v) {
+        if (token(g, e) < t.count) *reinterpret_cast<four*>(out + (long long)(t.first + token(g, e)) * a.out_stride) = v;
+    };
     if (t.adapter < 0) {
         if (a.y == a.out) return;
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            if (16 * g + l15 >= t.count) continue;
-            Sixteen<T> v;
-            v.load(y + row_of(g) * a.y_stride, lk);
-            const f32x4 same[4] = {v.four(0), v.four(1), v.four(2), v.four(3)};
-            Sixteen<T>::store(out + row_of(g) * a.out_stride, lk, same);
+            four v[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = load(g, e);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store(g, e, v[e]);
         }
         return;
     }
     struct Group {
-        Sixteen<T> v;
+        four v[4];
         f32x4 u[KS][2];
     };
     // ranks past the end, of which the products must see zeros on both sides (infinities and NaN), are copies of the last until then
-    const bool cut = (a.rank & 31) != 0;
+    const int pieces = a.rank >> 3;
+    const bool cut = (pieces & 3) != 0;
     auto fetch = [&](int g) {
         Group x;
-        x.v.load(y + row_of(g) * a.y_stride, lk);
-        const float* const p = a.u + row_of(g) * a.u_ranks;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x.v[e] = load(g, e);
 #pragma unroll
         for (int k = 0; k < KS; ++k)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) x.u[k][h] = *reinterpret_cast<const f32x4*>(p + min(32 * k + 8 * lk, a.u_ranks - 8) + 4 * h);
+            for (int h = 0; h < 2; ++h) x.u[k][h] = *reinterpret_cast<const f32x4*>(u_at(a, 0, t.slot + g, 8 * min(4 * k + lk, pieces - 1) + 4 * h, l15));
         if (NG == 1) {
-            for (int part = 1; part < a.parts; ++part) {
-                const float* const o = p + (long long)part * a.n_tokens * a.u_ranks;
+            for (int part = 1; part < a.parts; ++part)
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) x.u[k][h] += *reinterpret_cast<const f32x4*>(o + min(32 * k + 8 * lk, a.u_ranks - 8) + 4 * h);
-            }
+                    for (int h = 0; h < 2; ++h) x.u[k][h] += *reinterpret_cast<const f32x4*>(u_at(a, part, t.slot, 8 * min(4 * k + lk, pieces - 1) + 4 * h, l15));
         }
         return x;
     };
-    Group next = fetch(0);
+    // a row of B to row (column & 3) * 16 + column / 4 of the stage, whose rows are an odd number of pieces apart
     bf16x8 w[4][KS];
+    bf16x8* const mine = stage[wave];
+    const int apart = pieces | 1;
+    {
+        const bf16x8* const p = reinterpret_cast<const bf16x8*>(a.b + ((long long)t.adapter * a.N + block * 64) * a.rank);
+        bf16x8 v[4 * KS];
 #pragma unroll
-    for (int m = 0; m < 4; ++m) {
-        const bf16* const p = a.b + ((long long)t.adapter * a.N + block * 64 + Sixteen<T>::column(m, l15)) * a.rank;
+        for (int j = 0; j < 4 * KS; ++j)
+            if (j < pieces) v[j] = p[64 * j + lane];
+        const int per = (65536 + pieces - 1) / pieces;         // (quotients of numbers under 1024 by at most 16 are exact so)
 #pragma unroll
-        for (int k = 0; k < KS; ++k) w[m][k] = *reinterpret_cast<const bf16x8*>(p + min(32 * k + 8 * lk, a.rank - 8));
+        for (int j = 0; j < 4 * KS; ++j)
+            if (j < pieces) {
+                const int i = 64 * j + lane, column = (i * per) >> 16;
+                mine[((column & 3) * 16 + (column >> 2)) * apart + i - column * pieces] = v[j];
+            }
     }
-    __builtin_amdgcn_sched_barrier(0);
+    Group next = fetch(0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");     // (other lanes' writes)
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int k = 0; k < KS; ++k) w[m][k] = mine[(16 * m + l15) * apart + min(4 * k + lk, pieces - 1)];
     const bf16x8 none = {};
     if (cut) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) w[m][KS - 1] = 32 * (KS - 1) + 8 * lk < a.rank ? w[m][KS - 1] : none;
+        for (int m = 0; m < 4; ++m) w[m][KS - 1] = 4 * (KS - 1) + lk < pieces ? w[m][KS - 1] : none;
     }
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -220,10 +301,12 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
         Group now = next;
         if (g + 1 < NG && 16 * (g + 1) < t.count) next = fetch(g + 1);
         __builtin_amdgcn_sched_barrier(0);
-        if (cut && 32 * (KS - 1) + 8 * lk >= a.rank) now.u[KS - 1][0] = now.u[KS - 1][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (cut && 4 * (KS - 1) + lk >= pieces) now.u[KS - 1][0] = now.u[KS - 1][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         f32x4 acc[4];
 #pragma unroll
-        for (int m = 0; m < 4; ++m) acc[m] = now.v.four(m);
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[m][e] = (float)now.v[e][m];
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             bf16x8 piece[NP];
@@ -239,9 +322,15 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
 #pragma unroll
             for (int h = NP - 1; h >= 0; --h)
 #pragma unroll
-                for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[m][k], piece[h], acc[m], 0, 0, 0);
+                for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(piece[h], w[m][k], acc[m], 0, 0, 0);
         }
-        if (16 * g + l15 < t.count) Sixteen<T>::store(out + row_of(g) * a.out_stride, lk, acc);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            four v;
+#pragma unroll
+            for (int m = 0; m < 4; ++m) v[m] = (T)acc[m][e];
+            store(g, e, v);
+        }
     }
 }
 
@@ -295,11 +384,9 @@ __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned g
         if (adapted) {
             f32x4 u[2] = {};
             if (there)
-                for (int p = 0; p < a.parts; ++p) {
-                    const f32x4* const up = reinterpret_cast<const f32x4*>(a.u + ((long long)p * a.n_tokens + row) * a.u_ranks + 8 * piece);
-                    u[0] += up[0];
-                    u[1] += up[1];
-                }
+                for (int p = 0; p < a.parts; ++p)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) u[h] += *reinterpret_cast<const f32x4*>(u_row(a, p, t.first + i, 8 * piece + 4 * h));
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll
@@ -331,7 +418,7 @@ void launch_up_tiles(const LoraArgs& a, hipStream_t s) {
 }
 template <typename T>
 void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
-    if (max_q_len == 1) {
+    if (max_q_len <= 1) {
         auto go = [&](auto kernel, int blocks) {
             const unsigned groups = (unsigned)(a.N / 64 + 4 * blocks - 1) / (4 * blocks);
             hipLaunchKernelGGL(kernel, dim3(groups * (unsigned)(a.n_tokens / 16 + a.n_seqs)), dim3(256), 0, s, a, groups);
@@ -346,12 +433,6 @@ void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
     if (max_q_len <= 16) launch_up_tiles<T, 16>(a, s);
     else launch_up_tiles<T, 32>(a, s);
 }
-template <int NT, int RT>
-void launch_down(const LoraArgs& a, hipStream_t s) {
-    const unsigned groups = (unsigned)(a.u_ranks + 16 * RT - 1) / (16 * RT);
-    hipLaunchKernelGGL((lora_down_kernel<NT, RT>), dim3(groups * a.parts * (unsigned)(a.n_tokens / (16 * NT) + a.n_seqs)), dim3(64 * kDownWaves), 0, s, a, groups);
-}
-
 }  // namespace
 
 int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
@@ -361,10 +442,18 @@ int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
 }
 
 hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
-    const bool few = max_q_len <= 16;
-    if (few) launch_down<1, 1>(a, s);
-    else if (a.n_tokens < 4096 || a.u_ranks < 64) launch_down<2, 2>(a, s);
-    else launch_down<2, 4>(a, s);
+    if (max_q_len <= 16) {
+        const unsigned groups = (unsigned)(a.u_ranks / 16);
+        hipLaunchKernelGGL(lora_down_kernel, dim3(groups * a.parts * (unsigned)(a.n_tokens / 16 + a.n_seqs)), dim3(64 * kDownWaves), 0, s, a, groups);
+    } else {
+        auto go = [&](auto kernel, int ranks) {
+            const unsigned groups = (unsigned)((a.u_ranks + ranks - 1) / ranks);
+            hipLaunchKernelGGL(kernel, dim3(groups * (unsigned)(a.n_tokens / 32 + a.n_seqs)), dim3(256), 0, s, a, groups);
+        };
+        if (a.u_ranks <= 16) go(lora_down_tile_kernel<1>, 16);
+        else if (a.u_ranks <= 32) go(lora_down_tile_kernel<2>, 32);
+        else go(lora_down_tile_kernel<4>, 64);
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.fp32) launch_up<float>(a, max_q_len, s);

@@ -149,9 +149,10 @@ struct LoraArgs {
     void* out;
     long long x_stride, y_stride, out_stride;
     int n_seqs, n_tokens, K, N, rank, n_adapters, fp32;
-    float* u;                         // scale x A^T, K in parts: [parts][n_tokens][u_ranks]
+    float* u;                         // scale x A^T, K in parts: [parts][slots][u_ranks / 4][16 tokens][4]
     int u_ranks;                      // rank rounded up to 16
     int parts;
+    int slots;                        // sixteens of tokens of one sequence each; 0: u is [parts][n_tokens][u_ranks]
 };
 // parts of K: n_seqs, n_tokens, max_q_len, K, rank
 int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank);
