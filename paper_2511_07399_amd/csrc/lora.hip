@@ -1,14 +1,16 @@
 // Low-rank adapters of many requests beside a shared projection:  out = y + scale (x A^T) B^T, each sequence with its own A [r, K],
 // B [N, r] and scale, or none.
 //
-// Memory bound: x, y, out and the adapters' matrices once, 2 r (K + N) flops a row.  Two launches with u = scale x A^T between them; both
-// are products on 16x16x32 matrix instructions whose fragments come straight from memory (sixteen rows, 64 bytes each), since
-// nothing is used often enough to pay for its way through LDS.
-//   u: computed transposed, ranks as rows and tokens as columns.  A workgroup has 16 or 32 tokens of one sequence and 16 RT ranks; its eight
-//     waves take pieces of 64 of K in turn and add up through LDS.  u is left in 32 bits, and goes to the second product as two or three
-//     bf16 numbers that add up to it (kPieces: as one, its rounding would be the result's largest error).
-//   out: columns of out as rows, tokens as columns, y as the accumulator's start.  The rows of four instructions are interleaved so that a
-//     lane ends up with sixteen columns next to each other of its token.
+// Memory bound: x, y, out and the adapters' matrices once, 2 r (K + N) flops a row.  Two launches with u = scale x A^T between them, both
+// on 16x16x32 matrix instructions.  (One launch for both, each workgroup of the second product waiting for nothing but computing u again
+// or joined by a count, was slower wherever a sequence has few rows: 8 tokens of rank 64, 5120 x 5120, 12 us in two launches, 36 in one.)
+//   u: computed transposed, ranks as rows and tokens as columns.  Few tokens: lora_down_kernel, 16 tokens and 16 ranks a
+//     workgroup, its eight waves in turn over pieces of 64 of K, K in parts over workgroups.  Many: lora_down_tile_kernel, 32 tokens.  u stays in 32 bits, and goes to the second product as two or three bf16 numbers that add up to it
+//     (kPieces: as one, its rounding would be the result's largest error).
+//   out: lora_up_kernel, tokens as rows, y as the accumulator's start; one token a sequence: lora_up_few_kernel, on the vector unit.
+// What the cache is asked for a load decides: 16 bytes of a lane are an access by themselves unless the lanes next to it are in the same
+// line.  8800 tokens of four sequences, bf16, 5120 x 5120 of rank 64: fragments straight from memory 145 us, rows by lines through LDS 97
+// (270 MB in 46 + 53 us, 2.7 TB/s); 1536 x 1536 45 -> 32; 32 bits, 5120 x 5120, 175 -> 119 (3.8 TB/s).
 #include "ragged.h"
 
 namespace sdv2 {
@@ -51,40 +53,30 @@ template <typename T>
 constexpr int kPieces = sizeof(T) == 4 ? 3 : 2;
 
 __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, unsigned groups) {
-    __shared__ f32x4 parts[kDownWaves][1][64];
-    constexpr int NT = 1, RT = 1;
+    __shared__ f32x4 parts[kDownWaves][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l15 = lane & 15, lk = lane >> 4;
     const unsigned rest = blockIdx.x / a.parts, part = blockIdx.x - rest * a.parts, tile = rest / groups;
     Tile t;
-    if (!locate<16 * NT>(a, (int)tile, &t) || t.adapter < 0) return;
-    const int rank0 = (int)(rest - tile * groups) * (16 * RT);
+    if (!locate<16>(a, (int)tile, &t) || t.adapter < 0) return;
+    const int rank0 = (int)(rest - tile * groups) * 16;
     const float scale = a.scale != nullptr ? a.scale[t.adapter] : 1.0f;
 
-    const bf16 *wp[RT], *xp[NT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i) wp[i] = a.a + ((long long)t.adapter * a.rank + min(rank0 + 16 * i + l15, a.rank - 1)) * a.K + 8 * lk;
-#pragma unroll
-    for (int i = 0; i < NT; ++i) xp[i] = a.x + (long long)(t.first + min(16 * i + l15, t.count - 1)) * a.x_stride + 8 * lk;
-    f32x4 acc[RT][NT];
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    const bf16* const wp = a.a + ((long long)t.adapter * a.rank + min(rank0 + l15, a.rank - 1)) * a.K + 8 * lk;
+    const bf16* const xp = a.x + (long long)(t.first + min(l15, t.count - 1)) * a.x_stride + 8 * lk;
+    f32x4 acc = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     // pieces of 64 numbers (a line of 128 bytes in a row); several at once, so that their loads are in flight together
     constexpr int kAtOnce = 3;
     const int all = a.K >> 6, pieces = (int)((long long)all * (part + 1) / a.parts);
     for (int p0 = (int)((long long)all * part / a.parts) + wave; p0 < pieces; p0 += kDownWaves * kAtOnce) {
-        bf16x8 w[kAtOnce][2][RT], x[kAtOnce][2][NT];
+        bf16x8 w[kAtOnce][2], x[kAtOnce][2];
 #pragma unroll
         for (int c = 0; c < kAtOnce; ++c) {
             const int at = min(p0 + kDownWaves * c, pieces - 1) * 64;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < RT; ++i) w[c][h][i] = *reinterpret_cast<const bf16x8*>(wp[i] + at + 32 * h);
-#pragma unroll
-                for (int j = 0; j < NT; ++j) x[c][h][j] = *reinterpret_cast<const bf16x8*>(xp[j] + at + 32 * h);
+                w[c][h] = *reinterpret_cast<const bf16x8*>(wp + at + 32 * h);
+                x[c][h] = *reinterpret_cast<const bf16x8*>(xp + at + 32 * h);
             }
         }
         __builtin_amdgcn_sched_barrier(0);       // (left to itself, the compiler puts each load in front of its product)
@@ -92,31 +84,23 @@ __global__ __launch_bounds__(64 * kDownWaves) void lora_down_kernel(LoraArgs a, 
         for (int c = 0; c < kAtOnce; ++c) {
             if (p0 + kDownWaves * c >= pieces) break;
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c][h][i], x[c][h][j], acc[i][j], 0, 0, 0);
+            for (int h = 0; h < 2; ++h) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[c][h], x[c][h], acc, 0, 0, 0);
         }
     }
-#pragma unroll
-    for (int i = 0; i < RT; ++i)
-#pragma unroll
-        for (int j = 0; j < NT; ++j) parts[wave][i * NT + j][lane] = acc[i][j];
+    parts[wave][lane] = acc;
     __syncthreads();
-    for (int b = wave; b < RT * NT; b += kDownWaves) {
-        f32x4 u = parts[0][b][lane];
+    if (wave != 0) return;
+    f32x4 u = parts[0][lane];
 #pragma unroll
-        for (int k = 1; k < kDownWaves; ++k) u += parts[k][b][lane];
-        const int rank = rank0 + 16 * (b / NT) + 4 * lk, token = 16 * (b % NT) + l15;      // four ranks of one token
-        if (token >= t.count || rank >= a.u_ranks) continue;
+    for (int k = 1; k < kDownWaves; ++k) u += parts[k][lane];
+    const int rank = rank0 + 4 * lk;             // four ranks of one token
+    if (l15 >= t.count) return;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
-        *reinterpret_cast<f32x4*>(a.slots != 0 ? u_at(a, part, t.slot + (b % NT), rank, l15) : u_row(a, part, t.first + token, rank)) = u;
-    }
+    for (int e = 0; e < 4; ++e) u[e] = rank < a.rank ? u[e] * scale : 0.0f;
+    *reinterpret_cast<f32x4*>(a.slots != 0 ? u_at(a, part, t.slot, rank, l15) : u_row(a, part, t.first + l15, rank)) = u;
 }
 
-// The same for 32 tokens of a longer sequence and up to 64 ranks (16 RT), through LDS: a row's line of 128 bytes goes to eight lanes next
+// The same for 32 tokens and up to 64 ranks (16 RT), through LDS: a row's line of 128 bytes goes to eight lanes next
 // to each other, where a fragment's lanes next to each other have different rows, each an access of the cache by itself.  Each wave has
 // a stage of its own, and two pieces of 64 of K on their way to its registers.
 template <int RT>
@@ -405,6 +389,13 @@ __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned g
     }
 }
 
+// Tiles of sixteen tokens and ranks, K in parts, for one token a sequence and wherever that is under half a workgroup a compute unit; else
+// tiles of 32 tokens by lines.  Measured, by sixteens | by 32 in us, 5120 x 5120: 16 sequences of 4 tokens of rank 16 10.0 | 13.5, of 48
+// 13.9 | 19.5; one of 1000 of rank 128 38.7 | 32.6; 128 of 16 of rank 16 30.2 | 25.6; 1536 x 4608: 100 of 4 14.7 | 15.5, of 16 17.5 | 17.4,
+// 64 of 24 of rank 64 26.0 | 23.1, 64 of 16 19.6 | 20.1.
+int sixteens(int n_seqs, int n_tokens, int rank) { return max(n_tokens / 16, n_seqs) * ((rank + 15) / 16); }
+bool by_sixteens(int n_seqs, int n_tokens, int max_q_len, int rank) { return max_q_len <= 1 || sixteens(n_seqs, n_tokens, rank) < kUnits / 2; }
+
 template <typename T, int TOKENS>
 void launch_up_tiles(const LoraArgs& a, hipStream_t s) {
     const unsigned groups = (unsigned)(a.N / 64 + 3) / 4;
@@ -418,6 +409,8 @@ void launch_up_tiles(const LoraArgs& a, hipStream_t s) {
 }
 template <typename T>
 void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
+    // (by lanes | by tiles: 64 sequences of one token 15.2 | 18.4 us, of two 14.9 | 16.3; 16 of one, 5120 x 5120, 9.1 | 9.2, of two 9.6 | 9.3,
+    // of four 11.6 | 9.5)
     if (max_q_len <= 1) {
         auto go = [&](auto kernel, int blocks) {
             const unsigned groups = (unsigned)(a.N / 64 + 4 * blocks - 1) / (4 * blocks);
@@ -430,19 +423,19 @@ void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
         else go(lora_up_few_kernel<T, 16>, 1);
         return;
     }
-    if (max_q_len <= 16) launch_up_tiles<T, 16>(a, s);
+    if (by_sixteens(a.n_seqs, a.n_tokens, max_q_len, a.rank)) launch_up_tiles<T, 16>(a, s);
     else launch_up_tiles<T, 32>(a, s);
 }
 }  // namespace
 
 int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
-    if (max_q_len > 16) return 1;
-    const int workgroups = max(n_tokens / 16, n_seqs) * ((rank + 15) / 16);
-    return max(1, min(min(kUnits / workgroups, K / 1024), 4));
+    if (!by_sixteens(n_seqs, n_tokens, max_q_len, rank)) return 1;
+    // (1 part | these, 5120 x 5120 of rank 16: one token 12.7 | 8.6 us, 16 sequences of 8 15.6 | 9.9)
+    return max(1, min(min(kUnits / sixteens(n_seqs, n_tokens, rank), K / 1024), 4));
 }
 
 hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s) {
-    if (max_q_len <= 16) {
+    if (by_sixteens(a.n_seqs, a.n_tokens, max_q_len, a.rank)) {
         const unsigned groups = (unsigned)(a.u_ranks / 16);
         hipLaunchKernelGGL(lora_down_kernel, dim3(groups * a.parts * (unsigned)(a.n_tokens / 16 + a.n_seqs)), dim3(64 * kDownWaves), 0, s, a, groups);
     } else {

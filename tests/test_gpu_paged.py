@@ -491,7 +491,9 @@ def test_rows_of_no_batch_touch_nothing_outside(starts):
     ([1], 64, 64, 8, 1, False, False), ([1] * 9, 1536, 4608, 16, 4, False, True), ([5, 0, 40, 1, 130], 320, 448, 24, 3, True, True),
     ([300, 77], 512, 128, 64, 2, True, False), ([64, 200, 1], 128, 1024, 128, 3, False, False), ([3] * 100, 256, 192, 32, 7, False, True),
     ([1, 2], 5120, 640, 16, 2, True, False), ([1] * 5, 1024, 320, 128, 3, True, False), ([1, 7, 16], 640, 192, 40, 2, False, False),
-    ([9] * 300, 128, 64, 64, 5, True, True), ([2], 704, 2112, 72, 1, False, True)])
+    ([9] * 300, 128, 64, 64, 5, True, True), ([2], 704, 2112, 72, 1, False, True),
+    ([2000, 0, 70, 1], 128, 128, 16, 2, False, True), ([500, 0, 601], 192, 192, 72, 2, True, False), ([900, 130], 576, 64, 40, 2, False, False),
+    ([1100, 33], 64, 320, 8, 2, True, False), ([1] * 20, 256, 640, 24, 3, False, False), ([1, 0, 1] * 30, 192, 704, 64, 3, True, True)])
 def test_lora(q_len, K, N, rank, n, fp32, in_place):
     starts = [0] + list(np.cumsum(q_len))
     T = int(starts[-1]) + 2
