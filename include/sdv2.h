@@ -632,9 +632,9 @@ int32_t sdv2_paged_append(const sdv2_paged_cfg* cfg, void* k_pages_dev, void* v_
  *       j < e   and   (window = 0 or j >= e - window or j < sink),
  *       e = L for block 0 (a chunk sees every token, its own included);  e = min(L, (p / block + 1) block) otherwise: block 1 is the
  *       causal mask, block = tokens of a frame the frame-causal one.
- *   A row that sees nothing is the zero row.  What keys and values hold where a row does not see them (infinities, NaN, storage never
+ *   A row that sees nothing, or whose scores are all minus infinity, is the zero row.  What keys and values hold where a row does not see them (infinities, NaN, storage never
  *   written) does not reach it.
- *   scale <= 0: 1 / sqrt(128).  o overlaps none of what is read.
+ *   scale <= 0: 1 / sqrt(128).  Scores (scale q k) of up to 2^29 in size.  o overlaps none of what is read.
  * sdv2_paged_attention_workspace_bytes: for few rows and many keys, which are then shared out over the chip (0 where they are not).
  * ------------------------------------------------------------------------------------------------ */
 typedef struct sdv2_attn_mask {
@@ -654,8 +654,9 @@ int32_t sdv2_paged_attention(const sdv2_paged_cfg* cfg, const void* k_pages_dev,
  *     out[t] = y[t] + scale[i] (x[t] A_i^T) B_i^T,   i = adapter[s] of the row's sequence s;
  *   an id outside [0, n_adapters) is no adapter: out[t] = y[t].  x: bf16 rows of K; A: bf16 [n_adapters][rank][K]; B: bf16
  *   [n_adapters][N][rank]; scale: dev fp32 [n_adapters] or NULL (1); adapter: dev int32 [n_seqs]; q_start as in a ragged batch.
- *   y, out: rows of N, bf16 (out_fp32 = 0) or fp32 (1); out may be y, and overlaps nothing else that is read.  Sums are held in 32 bits; x A^T goes to the second product in
- *   32 bits, or as two (bf16 rows) or three (fp32 rows) bf16 numbers that add up to it.  K and N multiples of 64, rank a multiple of 8 up to 128.
+ *   y, out: rows of N, bf16 (out_fp32 = 0) or fp32 (1); out may be y, and overlaps nothing else that is read.  Sums are held in 32
+ *   bits; x A^T goes to the second product in 32 bits, or as two (bf16 rows) or three (fp32 rows) bf16 numbers that add up to it.  K and
+ *   N multiples of 64, rank a multiple of 8 up to 128.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct sdv2_lora_cfg {
     uint32_t struct_size;

@@ -71,7 +71,7 @@ def positions(seed, T, axes, far):
 @pytest.mark.parametrize("T,q_heads,k_heads,axes,halves,far,norm", [
     (1, 1, 1, 1, False, 10, True), (1, 32, 8, 1, True, 1 << 30, True), (7, 5, 3, 3, True, 300, True), (33, 12, 12, 3, False, 2000, True),
     (130, 40, 8, 1, True, 1000000, False), (3, 2, 1, 0, False, 1, True), (1500, 6, 2, 1, False, 50, True), (2, 9, 0, 3, False, 5, False),
-    (5, 0, 2, 1, True, 5, True), (600, 40, 40, 3, False, 300, True)])
+    (5, 0, 2, 1, True, 5, True), (600, 40, 40, 3, False, 300, True), (1700, 40, 37, 3, False, 300, True), (3500, 18, 5, 1, True, 9000, True)])
 def test_norm_rope(T, q_heads, k_heads, axes, halves, far, norm):
     qkv = randn(1, T, (q_heads + 2 * k_heads + 1) * D)              # rows with a gap between them
     g_q, g_k = (1.0 + randn(2, 2, D, dtype=torch.float32, scale=0.2)).unbind(0)
@@ -165,6 +165,8 @@ class Cache:
     ([5, 9], [3, 9], 3, 3, 64, False, 0, False, False),        # more new tokens than tokens: the first two have no place
     ([700, 500], [900, 500], 12, 12, 256, False, 3, False, True),
     ([2] * 150, list(range(2, 152)), 8, 1, 16, True, 1, True, True),
+    ([1900, 1, 300], [2000, 70, 300], 12, 12, 64, False, 3, False, True),
+    ([2600], [2590], 11, 5, 16, True, 1, True, True),
 ])
 def test_append(q_len, kv_len, q_heads, kv_heads, page, e4m3, axes, halves, norm):
     c = Cache(q_len, kv_len, kv_heads, page, e4m3, seed=3, pad_tokens=3)
@@ -395,6 +397,22 @@ def test_attention_with_large_scores():
     want, mass = attention_64(c, q, 2, 1, 0, 0)
     # scores up to 227 in 32 bits: 327 in the exponent of 2, whose error of 2^-15 (scale and product rounded) moves p by 2^-15
     close(o, want, BF16 * want.abs() + (BF16 + 2.0 ** -12) * mass, "large scores")
+
+
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_scores_far_below_zero(form):
+    """Of -2^28 and less: the largest of them takes everything."""
+    c = Cache([3], [100], 1, 16, seed=4).fill(2)
+    q = torch.zeros(3, D, dtype=torch.bfloat16, device="cuda")
+    q[:, 0] = -(2.0 ** 15)
+    best = 37                                   # the others' numbers are 2^9 and more away, their scores 2^20
+    for j in range(100):
+        page, slot = c.table[0, j // 16], j % 16
+        c.k[page, 0, slot] = 0.0
+        c.k[page, 0, slot, 0] = 2.0 ** 16 * (1.0 + ((j - best) % 100) / 128.0)
+    o = run_attention(c, q, 1, 0, 0, 0)
+    want = c.v[c.table[0, best // 16], 0, best % 16].double().cpu().expand(3, D)
+    close(o, want, 2 * BF16 * want.abs())       # p to bf16, the result to bf16
 
 
 def test_attention_offsets_beyond_32_bits():
