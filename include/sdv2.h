@@ -566,6 +566,7 @@ int32_t sdv2_attention_bf16(const void* q_dev, const void* const* k_dev, const v
  *   numbers is read as it lies, so that one appended token is 256 (128) bytes in a row per head.
  * Rows (q, k, v, o, x, y, out) are heads (columns) in a row of their own, `stride` elements from row to row.  Addresses are multiples
  *   of 16 bytes and strides multiples of 8 elements, so views into the rows of a projection's output serve as they are.
+ * A workspace belongs to one call at a time: calls that may overlap (on other streams, in other recorded graphs) have one each.
  * All of them: n_tokens = 0 is a batch without work (SDV2_OK, nothing launched).
  * Errors: null pointers, wrong sizes, misaligned addresses, strides shorter than a row: SDV2_INVALID_ARG; SDV2_WORKSPACE_TOO_SMALL.
  * ------------------------------------------------------------------------------------------------ */

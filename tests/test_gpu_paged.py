@@ -512,7 +512,8 @@ def test_rows_of_no_batch_touch_nothing_outside(starts):
     ([9] * 300, 128, 64, 64, 5, True, True), ([2], 704, 2112, 72, 1, False, True),
     ([2000, 0, 70, 1], 128, 128, 16, 2, False, True), ([500, 0, 601], 192, 192, 72, 2, True, False), ([900, 130], 576, 64, 40, 2, False, False),
     ([1100, 33], 64, 320, 8, 2, True, False), ([1] * 20, 256, 640, 24, 3, False, False), ([1, 0, 1] * 30, 192, 704, 64, 3, True, True)])
-def test_lora(q_len, K, N, rank, n, fp32, in_place):
+def test_lora(q_len, K, N, rank, n, fp32, in_place, bound=None):
+    bound = max(q_len) if bound is None else bound
     starts = [0] + list(np.cumsum(q_len))
     T = int(starts[-1]) + 2
     x = randn(1, T, K + 64)[:, :K]
@@ -522,9 +523,9 @@ def test_lora(q_len, K, N, rank, n, fp32, in_place):
     y = randn(5, T, N + 32, dtype=torch.float32 if fp32 else torch.bfloat16)[:, :N]
     out = y if in_place else torch.full((T, N), 4.0, dtype=y.dtype, device="cuda")
     y0 = y.clone()
-    need = b.lora_workspace_bytes(len(q_len), T, max(q_len), K, rank)
+    need = b.lora_workspace_bytes(len(q_len), T, bound, K, rank)
     ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda") if need else None
-    b.lora_bf16(x, a, w, scale, ints(ids), ints(starts), max(q_len), y, out, ws)
+    b.lora_bf16(x, a, w, scale, ints(ids), ints(starts), bound, y, out, ws)
     want = y0.double().cpu()
     err = torch.zeros_like(want)
     for i, (m, idx) in enumerate(zip(q_len, ids)):
@@ -544,6 +545,12 @@ def test_lora(q_len, K, N, rank, n, fp32, in_place):
     for i, idx in enumerate(ids):
         if not 0 <= idx < n:
             assert torch.equal(out[starts[i]:starts[i + 1]], y0[starts[i]:starts[i + 1]])
+
+
+@pytest.mark.parametrize("bound", [0, 1, 5])
+def test_adapters_of_sequences_longer_than_stated(bound):
+    test_lora([40, 3, 0, 17], 320, 448, 24, 3, True, True, bound)
+    test_lora([1100, 33], 64, 320, 72, 2, False, False, bound)
 
 
 # ------------------------------------------------------------------------------------------ together
