@@ -633,8 +633,8 @@ int32_t sdv2_paged_append(const sdv2_paged_cfg* cfg, void* k_pages_dev, void* v_
  *       j < e   and   (window = 0 or j >= e - window or j < sink),
  *       e = L for block 0 (a chunk sees every token, its own included);  e = min(L, (p / block + 1) block) otherwise: block 1 is the
  *       causal mask, block = tokens of a frame the frame-causal one.
- *   A row that sees nothing, or whose scores are all minus infinity, is the zero row.  What keys and values hold where a row does not see them (infinities, NaN, storage never
- *   written) does not reach it.
+ *   A row that sees nothing, or whose scores are all minus infinity, is the zero row.  What keys and values hold where a row does not
+ *   see them (infinities, NaN, storage never written) does not reach it.
  *   scale <= 0: 1 / sqrt(128).  Scores (scale q k) of up to 2^29 in size.  o overlaps none of what is read.
  * sdv2_paged_attention_workspace_bytes: for few rows and many keys, which are then shared out over the chip (0 where they are not).
  * ------------------------------------------------------------------------------------------------ */

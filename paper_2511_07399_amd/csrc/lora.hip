@@ -1,12 +1,13 @@
 // Low-rank adapters of many requests beside a shared projection:  out = y + scale (x A^T) B^T, each sequence with its own A [r, K],
 // B [N, r] and scale, or none.
 //
-// Memory bound: x, y, out and the adapters' matrices once, 2 r (K + N) flops a row.  Two launches with u = scale x A^T between them, both
-// on 16x16x32 matrix instructions.  (One launch for both, each workgroup of the second product waiting for nothing but computing u again
-// or joined by a count, was slower wherever a sequence has few rows: 8 tokens of rank 64, 5120 x 5120, 12 us in two launches, 36 in one.)
-//   u: computed transposed, ranks as rows and tokens as columns.  Few tokens: lora_down_kernel, 16 tokens and 16 ranks a
-//     workgroup, its eight waves in turn over pieces of 64 of K, K in parts over workgroups.  Many: lora_down_tile_kernel, 32 tokens.  u stays in 32 bits, and goes to the second product as two or three bf16 numbers that add up to it
-//     (kPieces: as one, its rounding would be the result's largest error).
+// Memory bound: x, y, out and the adapters' matrices once, 2 r (K + N) flops a row.  Two launches with u = scale x A^T between them, on
+// 16x16x32 matrix instructions.  (One launch, in which each workgroup of the second product forms u for itself, reads A once per
+// workgroup: 64 tokens of rank 16, 5120 to 15 360, 12.3 us instead of 13.2, but 8 of rank 64, 5120 x 5120, 36 instead of 12.)
+//   u: computed transposed, ranks as rows and tokens as columns.  Few tokens: lora_down_kernel, 16 tokens and 16 ranks a workgroup, its
+//     eight waves in turn over pieces of 64 of K, K in parts over workgroups.  Many: lora_down_tile_kernel, 32 tokens.  u stays in 32
+//     bits, and goes to the second product as two or three bf16 numbers that add up to it (kPieces: as one, its rounding would be the
+//     result's largest error).
 //   out: lora_up_kernel, tokens as rows, y as the accumulator's start; one token a sequence: lora_up_few_kernel, on the vector unit.
 // What the cache is asked for a load decides: 16 bytes of a lane are an access by themselves unless the lanes next to it are in the same
 // line.  8800 tokens of four sequences, bf16, 5120 x 5120 of rank 64: fragments straight from memory 145 us, rows by lines through LDS 97
@@ -300,7 +301,8 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
 #pragma unroll
                 for (int h = 0; h < NP; ++h) {
                     piece[h][e] = (bf16)rest;
-                    rest -= (float)piece[h][e];
+                    const float less = rest - (float)piece[h][e];
+                    rest = less == less ? less : 0.0f;         // (of an infinity nothing is left)
                 }
             }
 #pragma unroll

@@ -547,6 +547,35 @@ def test_lora(q_len, K, N, rank, n, fp32, in_place, bound=None):
             assert torch.equal(out[starts[i]:starts[i + 1]], y0[starts[i]:starts[i + 1]])
 
 
+@pytest.mark.parametrize("q_len,fp32", [([1, 1], False), ([20, 9], True), ([20, 9], False), ([2100, 30], True), ([2100, 30], False)])
+def test_adapters_of_broken_rows(q_len, fp32):
+    """Infinities and NaN in x come out where the formula has them, in their own rows."""
+    K, N, rank, T = 128, 192, 8, sum(q_len)
+    x = randn(1, T, K)
+    a, w = randn(2, 2, rank, K, scale=0.1), randn(3, 2, N, rank, scale=0.3)
+    a[:, :, 3] = a[:, :, 3].abs() + 0.5         # x[:, 3] infinite: every u is, and of one sign
+    w[:, :64] = w[:, :64].abs() + 0.25
+    y = randn(5, T, N, dtype=torch.float32 if fp32 else torch.bfloat16)
+    bound, starts = max(q_len), ints([0, q_len[0], T])
+    ws = torch.empty(b.lora_workspace_bytes(2, T, bound, K, rank), dtype=torch.uint8, device="cuda")
+    clean, out = torch.empty_like(y), torch.empty_like(y)
+    b.lora_bf16(x, a, w, None, ints([0, 1]), starts, bound, y, clean, ws)
+    x[0, 3], x[T - 1, 3] = float("inf"), float("-inf")
+    if T > 2:
+        x[5, 7] = float("nan")
+    b.lora_bf16(x, a, w, None, ints([0, 1]), starts, bound, y, out, ws)
+    whole = torch.ones(T, dtype=torch.bool)
+    for t, i in ((0, 0), (T - 1, 1)):
+        whole[t] = False
+        want = y[t].double().cpu() + (x[t].double().cpu() @ a[i].double().cpu().t()) @ w[i].double().cpu().t()
+        got = out[t].double().cpu()
+        assert want[:64].isinf().all() and torch.equal(got.isnan(), want.isnan()) and torch.equal(got[~want.isnan()], want[~want.isnan()])
+    if T > 2:
+        whole[5] = False
+        assert out[5].isnan().all()
+    assert torch.equal(out.cpu()[whole], clean.cpu()[whole])
+
+
 @pytest.mark.parametrize("bound", [0, 1, 5])
 def test_adapters_of_sequences_longer_than_stated(bound):
     test_lora([40, 3, 0, 17], 320, 448, 24, 3, True, True, bound)
