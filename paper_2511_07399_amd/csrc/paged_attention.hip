@@ -13,6 +13,7 @@
 //     keys of 8 bits 179 GF in 210 us, the join's reading included.
 #include "ragged.h"
 
+#include <climits>
 #include <mutex>
 #include <type_traits>
 
@@ -829,12 +830,18 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
                 const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit);
                 if (lane == 0) flags[wave] = hits != 0;
                 const RowKeys keys = row_keys(a.mask, place_of(own_row()).token, w.n, w.kv_len);
+                // bounds relative to this lane's first key; sixteen keys without a page are behind the end
+                const int mine = key0 + 4 * lh, before = keys.end - mine, from = keys.low - mine, sink = keys.sink - mine;
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int j = kb * 32 + 8 * (r >> 2) + 4 * lh + (r & 3);
-                        if (!sees(keys, key0 + j) | (((gaps >> (2 * kb + (r >> 3))) & 1) != 0)) s_cur[kb][r] = -INFINITY;
+                    for (int half = 0; half < 2; ++half) {
+                        const int stop = (gaps >> (2 * kb + half)) & 1 ? INT_MIN : before;
+#pragma unroll
+                        for (int r = 8 * half; r < 8 * half + 8; ++r) {
+                            const int j = kb * 32 + 8 * (r >> 2) + (r & 3);
+                            if (j >= stop | (j < from & j >= sink)) s_cur[kb][r] = -INFINITY;
+                        }
                     }
             }
             const Source src = source_of(next_pages, n + kAhead, kAhead - 1);
