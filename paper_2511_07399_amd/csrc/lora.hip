@@ -369,10 +369,18 @@ __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned g
         for (int b = 0; b < kBlocks; ++b) x[b] = 0.0f;
         if (adapted) {
             f32x4 u[2] = {};
-            if (there)
-                for (int p = 0; p < a.parts; ++p)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) u[h] += *reinterpret_cast<const f32x4*>(u_row(a, p, t.first + i, 8 * piece + 4 * h));
+            if (there) {
+                auto at = [&](int p, int h) { return *reinterpret_cast<const f32x4*>(u_row(a, p, t.first + i, 8 * piece + 4 * h)); };
+                u[0] = at(0, 0);
+                u[1] = at(0, 1);
+                for (int p = 1; p < a.parts; p += 2) {        // (two parts, or three, on their way at once)
+                    const int q = min(p + 1, a.parts - 1);
+                    const f32x4 x = at(p, 0), y = at(p, 1), v = at(q, 0), z = at(q, 1);
+                    u[0] += x;
+                    u[1] += y;
+                    if (q > p) u[0] += v, u[1] += z;
+                }
+            }
 #pragma unroll
             for (int b = 0; b < kBlocks; ++b)
 #pragma unroll

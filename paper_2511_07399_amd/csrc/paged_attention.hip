@@ -840,7 +840,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
 #pragma unroll
                         for (int r = 8 * half; r < 8 * half + 8; ++r) {
                             const int j = kb * 32 + 8 * (r >> 2) + (r & 3);
-                            if (j >= stop | (j < from & j >= sink)) s_cur[kb][r] = -INFINITY;
+                            if ((j >= stop) | ((j < from) & (j >= sink))) s_cur[kb][r] = -INFINITY;
                         }
                     }
             }
