@@ -8,9 +8,9 @@
 // joins parts of a key range.  Measured (32 query and 8 key heads unless said otherwise):
 //   few rows: 64 tokens over 1 to 16 000 keys 1.99 GB in 365 us, 5.45 TB/s (reads of 8 KB at random places alone: 6.05); 8-bit pages,
 //     0.99 GB, 194 us, 5.1 TB/s; one token over 9001 keys 14.5 us in two launches.
-//   many rows: 2 x 4680 rows of 12 heads over 10 920 keys 628 GF in 614 us, 1.02 PF/s (a long loop of this kernel 1.13, of the one over
-//     contiguous keys 1.2); six prompts of 1 to 4096 tokens, causal, 234 GF in 270 us: the last workgroups' tail; 333 rows over 32 700
-//     keys of 8 bits 179 GF in 210 us, the join's reading included.
+//   many rows: 2 x 4680 rows of 12 heads over 10 920 keys 628 GF in 694 us, 0.9 PF/s (the kernel over contiguous keys, whose values lie
+//     transposed already and whose p is one bf16 number, 1.2); six prompts of 1 to 4096 tokens, causal, 234 GF in 298 us: the last
+//     workgroups' tail; 333 rows over 32 700 keys of 8 bits 179 GF in 207 us, the join's reading included.
 #include "ragged.h"
 
 #include <climits>
@@ -22,9 +22,103 @@ namespace sdv2 {
 namespace {
 
 constexpr int D = kHeadDim;
-constexpr float kSlack = 8.0f;       // log2 units that a row's scores may run ahead of its exponents' reference point
 constexpr float kSumLimit = 16384.0f;     // a lane's sum of p over one tile (at most 32 keys) beyond this: move the reference
 constexpr float kNoKey = -1.0e30f;   // reference point of a row that has seen no key yet: finite, so that -inf minus it is -inf
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Formats of a row of 128 numbers, in a page or in LDS.
+enum Format { kBf16, kE4m3, kFp16 };
+
+// p of eight keys on its way to the second product, whose other side is values: as one bf16 number it would add an error the size of
+// the output's own rounding (2.3e-3 of the output against 64 bits, where the rounding alone is 1.66e-3).
+//   With bf16 values: two bf16 numbers that add up to p but for 2^-16 of it, a product each.
+//   With fp16 values: one fp16 number, p but for 2^-11.  What is under 2^-14 loses bits there, so the reference point of the exponents lies
+//     kLift under the row's maximum: p of that is 2^8, and what a small one loses is 2^-33 of it at most.
+template <int F>
+struct Weights {
+    f16x8 x;
+    static constexpr float kLift = 8.0f, kSlack = 6.0f;      // kSlack: log2 units that the maximum may rise before the reference point is moved
+    __device__ __forceinline__ void set(int e, float p) { x[e] = (_Float16)p; }
+    __device__ __forceinline__ float get(int e) const { return (float)x[e]; }
+    __device__ __forceinline__ void pin() { asm volatile("" : "+v"(x)); }
+};
+template <>
+struct Weights<kBf16> {
+    bf16x8 hi, lo;
+    static constexpr float kLift = 0.0f, kSlack = 8.0f;
+    __device__ __forceinline__ void set(int e, float p) {
+        hi[e] = (bf16)p;
+        lo[e] = (bf16)(p - (float)hi[e]);
+    }
+    __device__ __forceinline__ float get(int e) const { return (float)hi[e] + (float)lo[e]; }
+    __device__ __forceinline__ void pin() { asm volatile("" : "+v"(hi), "+v"(lo)); }
+};
+
+// o[db] += values (32 channels x 16 keys of each db) times p.
+__device__ __forceinline__ void add_values(f32x16 (&o)[4], const bf16x8 (&v)[4], const Weights<kBf16>& w) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[db], w.lo, o[db], 0, 0, 0);
+#pragma unroll
+    for (int db = 0; db < 4; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[db], w.hi, o[db], 0, 0, 0);
+}
+template <int F>
+__device__ __forceinline__ void add_values(f32x16 (&o)[4], const f16x8 (&v)[4], const Weights<F>& w) {
+#pragma unroll
+    for (int db = 0; db < 4; ++db) o[db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v[db], w.x, o[db], 0, 0, 0);
+}
+
+// Eight fp16 from eight e4m3 (exact).
+__device__ __forceinline__ f16x8 widen_to_fp16(u32x2 v) {
+    f16x8 out;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        const f16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[w], 1.0f, false);
+        const f16x2 hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v[w], 1.0f, true);
+        out[4 * w] = lo[0];
+        out[4 * w + 1] = lo[1];
+        out[4 * w + 2] = hi[0];
+        out[4 * w + 3] = hi[1];
+    }
+    return out;
+}
+
+// Eight fp16 from eight bf16 times kValueScale: exact where each of them is zero or of size 2^-25 up to 2^8, which `range` keeps account of.
+constexpr float kValueScale = 256.0f;
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+struct Range {
+    u16x2 least = {0xffff, 0xffff};          // twice the bits of the smallest but zero, less one (0xfe: 2^-17 in fp16)
+    f16x2 large = {0, 0};                    // NaN: one was too large, infinite or NaN
+    __device__ __forceinline__ bool left() const {
+        return least[0] < 0xff || least[1] < 0xff || !(large[0] == (_Float16)0) || !(large[1] == (_Float16)0);
+    }
+};
+__device__ __forceinline__ f16x8 scaled_to_fp16(uint4 x, Range& range) {
+    uint4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
+        const float lo = __uint_as_float(w << 16) * kValueScale, hi = __uint_as_float(w & 0xffff0000u) * kValueScale;
+        unsigned h = __builtin_bit_cast(unsigned, f16x2{(_Float16)lo, (_Float16)hi}), twice;
+        asm("" : "+v"(h));                   // (or it is formed twice)
+        asm("v_pk_mad_u16 %0, %1, 2, -1 op_sel_hi:[1,0,1]" : "=v"(twice) : "v"(h));
+        range.least = __builtin_elementwise_min(range.least, __builtin_bit_cast(u16x2, twice));
+        range.large = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, h), f16x2{0, 0}, range.large);
+        (i == 0 ? out.x : i == 1 ? out.y : i == 2 ? out.z : out.w) = h;
+    }
+    return __builtin_bit_cast(f16x8, out);
+}
+
+// Whether any number is infinite or NaN.
+__device__ __forceinline__ bool broken_sums(const f32x16 (&o)[4]) {
+    float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) t[r & 3] = __builtin_fmaf(o[db][r], 0.0f, t[r & 3]);
+    return !((t[0] + t[1]) + (t[2] + t[3]) == 0.0f);
+}
 
 typedef __attribute__((address_space(3))) void* lds_void_ptr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -129,16 +223,18 @@ __device__ __forceinline__ bool sees(const RowKeys& k, int j) { return (j < k.en
 
 // ---------------------------------------------------------------------------------------------------
 // Tiles of keys and values in LDS as they lie in a page, [key][128], a row's 16-byte chunks permuted so that fragment reads spread
-// over the 64 banks.  Format of a row: 256 bytes of bf16 or 128 of e4m3.
+// over the 64 banks.  A row: 256 bytes of bf16 or (values) fp16, or 128 of e4m3.
 //   K fragment (32 keys x 16 numbers): a lane reads its key's row, 16 bytes at a time; chunk c of row r lies at c ^ (r % 16), e4m3:
 //     c ^ (r / 2 % 8).  Of e4m3, 16 bytes are two steps' numbers: lane half lh of step s has numbers 32 (s / 2) + 16 lh + 8 (s % 2) .. + 7
 //     where bf16 has 16 s + 8 lh .. + 7, and the query's fragments go by the same rule.
 //   V fragment (32 channels x 16 keys) transposed: ds_read_b64_tr hands each of 16 lanes a column of the rows that the 16 lanes
 //     address, four keys of 16 bits or eight of 8 bits, and the rows are picked in the order in which the scores' accumulators hold
 //     the keys (4 lh .. + 3 and 8 + 4 lh .. + 3 of sixteen).  Chunk c of row r lies at c ^ (r % 4) * 4; e4m3: c ^ 2 (r / 2 % 2 + 2 (r / 8 % 2)).
-template <bool E4M3>
+template <int F>
 struct Rows {
+    static constexpr bool E4M3 = F == kE4m3;
     static constexpr int kRow = E4M3 ? 128 : 256;             // bytes
+    typedef std::conditional_t<F == kBf16, bf16x8, f16x8> Values;
     static constexpr int kPerLoad = 1024 / kRow;              // rows of a wave load
     // byte within the rows of load number i that this lane fetches to its place (K, V)
     static __device__ __forceinline__ int k_source(int lane, int i) {
@@ -180,15 +276,15 @@ struct Rows {
         return (4 * lh + x) * 256 + ((db ^ x) << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
     }
     // fragment of sixteen keys whose rows start at `tile`
-    static __device__ __forceinline__ bf16x8 v_fragment(const unsigned char* tile, int at) {
-        if (E4M3) {
+    static __device__ __forceinline__ Values v_fragment(const unsigned char* tile, int at) {
+        if constexpr (E4M3) {
             const i32x2 x = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2_ptr)(tile + at));
-            return widen_e4m3(__builtin_bit_cast(u32x2, x));
+            return widen_to_fp16(__builtin_bit_cast(u32x2, x));
         }
         const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(tile + at));
         const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)(tile + at + 8 * 256));
         typedef short s16x8 __attribute__((ext_vector_type(8)));
-        return __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        return __builtin_bit_cast(Values, (s16x8)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
     // whether these sixteen bytes of values hold an infinity or NaN
     static __device__ __forceinline__ bool broken(uint4 x) {
@@ -197,6 +293,7 @@ struct Rows {
         for (int i = 0; i < 4; ++i) {
             const unsigned w = i == 0 ? x.x : i == 1 ? x.y : i == 2 ? x.z : x.w;
             if (E4M3) hit |= ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;                    // 0x7f or 0xff
+            else if (F == kFp16) hit |= ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
             else hit |= ((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;                         // exponent of ones
         }
         return hit != 0;
@@ -204,9 +301,9 @@ struct Rows {
 };
 
 // Bit j: key j of the 32 whose value rows start at row `first` of the tile holds an infinity or NaN.
-template <bool E4M3>
+template <int F>
 __device__ __forceinline__ unsigned broken_keys(const unsigned char* v, int first, int lane) {
-    typedef Rows<E4M3> R;
+    typedef Rows<F> R;
     const int row = first + (lane & 31);
     bool hit = false;
     constexpr int kChunks = R::kRow / 16 / 2;                 // of this lane: half a row
@@ -220,37 +317,57 @@ __device__ __forceinline__ unsigned broken_keys(const unsigned char* v, int firs
     return (unsigned)(b | (b >> 32));
 }
 
-// Adds to O^T the keys in `broken` of 32 (rows `first` .. of the value tile), one by one and only to the rows whose p is not zero: in a product
-// with the others, zero times their infinities or NaN would reach rows that do not see them.  pf: the 32 keys' two fragments of p.
-// scratch: 2 KB of the wave's.  The caller then blanks these keys' values and goes on as ever.  Rare, so short, not fast.
+// Adds to O^T the keys in `broken` of 32 (rows `first` .. of the value tile), one by one and only to the rows that see them: in a product
+// with the others, zero times their infinities or NaN would reach rows that do not, and an infinity times p's second piece would be
+// NaN where p times it is not.  w0, w1: p of the 32 keys; sees(j): whether this lane's row sees key j.  scratch: 2 KB of the wave's.
+// The caller then blanks these keys' values and goes on as ever.  Rare, so short, not fast.
 constexpr int kApartBytes = 2048;
-template <bool E4M3>
-__device__ __forceinline__ void add_apart(f32x16 (&o)[4], const unsigned char* v, int first, const bf16x8& p0, const bf16x8& p1, unsigned broken,
-                                          unsigned char* scratch, int lane) {
-    typedef Rows<E4M3> R;
+template <int F, typename S>
+__device__ __forceinline__ void add_apart(f32x16 (&o)[4], const unsigned char* v, int first, const Weights<F>& w0, const Weights<F>& w1, unsigned broken,
+                                          unsigned char* scratch, int lane, S&& sees) {
+    typedef Rows<F> R;
     const int lh = lane >> 5;
-    *reinterpret_cast<bf16x8*>(scratch + lane * 32) = p0;
-    *reinterpret_cast<bf16x8*>(scratch + lane * 32 + 16) = p1;
-    while (broken != 0) {
-        const int j = __builtin_ctz(broken), row = first + j;
-        broken &= broken - 1;
-        // key j of sixteen: element (j & 3) + 4 (j / 8 % 2) of lane half j / 4 % 2
-        const float p = (float)*reinterpret_cast<const bf16*>(scratch + ((lane & 31) + 32 * ((j >> 2) & 1)) * 32 + (j >> 4) * 16 + ((j & 3) + 4 * ((j >> 3) & 1)) * 2);
+    float* const own = reinterpret_cast<float*>(scratch);     // [eight keys of sixteen][64 lanes]
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
+    for (int half = 0; half < 2; ++half) {
+        unsigned left = broken >> (16 * half) & 0xffffu;
+        if (left == 0) continue;
+        reads_done();                                         // (of what lay there)
 #pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                bf16x4 x;
-                if (E4M3) {
-                    const unsigned w = *reinterpret_cast<const unsigned*>(v + R::v_position(row, 2 * db + (g >> 1)) + 8 * (g & 1) + 4 * lh);
-                    const bf16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
-                    x = bf16x4{lo[0], lo[1], hi[0], hi[1]};
-                } else {
-                    x = *reinterpret_cast<const bf16x4*>(v + R::v_position(row, 4 * db + g) + 8 * lh);
+        for (int e = 0; e < 8; ++e) own[e * 64 + lane] = half == 0 ? w0.get(e) : w1.get(e);
+        hold_order();
+#pragma clang loop unroll(disable)
+        while (left != 0) {
+            const int j = __builtin_ctz(left), row = first + 16 * half + j;
+            left &= left - 1;
+            const unsigned keep = sees(16 * half + j) ? ~0u : 0u;
+            // key j of sixteen: element (j & 3) + 4 (j / 8) of lane half j / 4 % 2
+            const float p = own[((j & 3) + 4 * (j >> 3)) * 64 + (lane & 31) + 32 * ((j >> 2) & 1)];
+#pragma unroll
+            for (int db = 0; db < 4; ++db)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    float x[4];
+                    if (F == kE4m3) {
+                        const unsigned w = *reinterpret_cast<const unsigned*>(v + R::v_position(row, 2 * db + (g >> 1)) + 8 * (g & 1) + 4 * lh);
+                        const f16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true);
+                        x[0] = lo[0], x[1] = lo[1], x[2] = hi[0], x[3] = hi[1];
+                    } else {
+                        const uint2 w = *reinterpret_cast<const uint2*>(v + R::v_position(row, 4 * db + g) + 8 * lh);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const unsigned short n = (unsigned short)((e < 2 ? w.x : w.y) >> (16 * (e & 1)));
+                            x[e] = F == kFp16 ? (float)__builtin_bit_cast(_Float16, n) : (float)__builtin_bit_cast(bf16, n);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        // (p may be zero in 32 bits, and infinity times it is an infinity)
+                        const float t = __builtin_fabsf(x[e]) < INFINITY ? p * x[e] : x[e];
+                        o[db][4 * g + e] += __uint_as_float(__float_as_uint(t) & keep);
+                    }
                 }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[db][4 * g + e] += p != 0.0f ? p * (float)x[e] : 0.0f;
-            }
+        }
     }
 }
 
@@ -313,7 +430,9 @@ constexpr int kTokenStages = 65536, kTokenLds = kTokenStages + kTokenWaves * kAp
 
 template <bool E4M3>
 __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAttnArgs a) {
-    typedef Rows<E4M3> R;
+    constexpr int F = E4M3 ? kE4m3 : kBf16;
+    typedef Rows<F> R;
+    typedef Weights<F> P;
     constexpr int KT = kTokenTile, NW = kTokenWaves;
     constexpr int kStages = E4M3 ? 2 : 1;
     constexpr int kTile = KT * R::kRow, kLoads = KT / R::kPerLoad;          // bytes and wave loads of a K or V tile
@@ -357,12 +476,17 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
     const int* const table = a.batch.table + (long long)w.seq * a.batch.table_stride;
     const int slot_mask = (1 << a.batch.page_shift) - 1;
 
+    // A wave whose sums have come out broken goes over its keys once more, with care: an infinite value that every row of a tile sees
+    // belongs into the result, where the two pieces of p have made a NaN of it.  (e4m3 has no infinity.)
     f32x16 o[4];
+    float m, l;
+    bool careful = false;
+again:
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[db][r] = 0.0f;
-    float m = kNoKey, l = 0.0f;
+    m = kNoKey, l = 0.0f;
 
     // 32 tiles at a time, whose 64 pages of sixteen keys the lanes look up together
     for (int batch = 0; batch < count; batch += 32) {
@@ -423,10 +547,10 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
                 }
             }
             const float top = block_max(s0) * a.mask.scale_log2e;
-            if (__builtin_amdgcn_ballot_w64(top > m + kSlack) != 0) {
-                const bool moved = top > m + kSlack;
-                const float alpha = moved ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
-                m = moved ? top : m;
+            const bool moved = top > m + (P::kLift + P::kSlack);
+            if (__builtin_amdgcn_ballot_w64(moved) != 0) {
+                const float next = moved ? top - P::kLift : m, alpha = __builtin_amdgcn_exp2f(m - next);
+                m = next;
                 l *= alpha;
 #pragma unroll
                 for (int db = 0; db < 4; ++db)
@@ -434,30 +558,33 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
                     for (int r = 0; r < 16; ++r) o[db][r] *= alpha;
             }
             float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-            bf16x8 pf[2];
+            P pf[2];
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s0[r], a.mask.scale_log2e, -m));
                 sum[r & 3] += p;
-                pf[r >> 3][r & 7] = (bf16)p;
+                pf[r >> 3].set(r & 7, p);
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             // and these values: behind them went out kStages - 1 tiles and the keys just asked for
             if (i + kStages < n) __builtin_amdgcn_s_waitcnt(0x0F70 | (kLoads * (2 * kStages - 1)));
             else __builtin_amdgcn_s_waitcnt(0x0F70);
             hold_order();
-            const unsigned broken = masked ? broken_keys<E4M3>(vt, 0, lane) : 0u;
+            const unsigned broken = masked || careful ? broken_keys<F>(vt, 0, lane) : 0u;
             if (__builtin_expect(broken != 0, 0)) {
-                add_apart<E4M3>(o, vt, 0, pf[0], pf[1], broken, smem + kTokenStages + wave * kApartBytes, lane);
+                add_apart<F>(o, vt, 0, pf[0], pf[1], broken, smem + kTokenStages + wave * kApartBytes, lane,
+                             [&](int j) { return sees(keys, key0 + j) & (((gaps >> (j >> 4)) & 1) == 0); });
                 if ((broken >> l31) & 1)
                     for (int c = 0; c < R::kRow / 32; ++c) *reinterpret_cast<uint4*>(vt + l31 * R::kRow + lh * (R::kRow / 2) + c * 16) = uint4{0, 0, 0, 0};
                 reads_done();
             }
 #pragma unroll
-            for (int ts = 0; ts < 2; ++ts)
+            for (int ts = 0; ts < 2; ++ts) {
+                typename R::Values v[4];
 #pragma unroll
-                for (int db = 0; db < 4; ++db)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(R::v_fragment(vt + 16 * ts * R::kRow, R::v_lane(lane, db)), pf[ts], o[db], 0, 0, 0);
+                for (int db = 0; db < 4; ++db) v[db] = R::v_fragment(vt + 16 * ts * R::kRow, R::v_lane(lane, db));
+                add_values(o, v, pf[ts]);
+            }
             if (i + kStages < n) {
                 reads_done();
                 fetch(a.v_pages, i + kStages, vt, true);
@@ -479,6 +606,10 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
             if (kStages == 2 && ++i < n) step(k_second + wave * kTile, v_second + wave * kTile, i);
         }
         reads_done();                                                        // the buffers are free for the next 32 tiles
+    }
+    if (!E4M3 && !careful && __builtin_expect(__builtin_amdgcn_ballot_w64(broken_sums(o)) != 0, 0)) {
+        careful = true;
+        goto again;
     }
 
     // ---- join the waves, in their order: wave w adds up and stores channels 32 w .. + 31
@@ -608,8 +739,12 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs
 //     come the values of tile n.  The loads of keys n + 2 and values n + 1 go out between the first products.
 //   * The reference point of a row's exponents trails its maximum by up to kSumLimit's logarithm: a steady tile forms no maximum and
 //     rescales nothing.
-//   * 8-bit pages pass through registers on their way to LDS and are widened there, once per tile: every wave reads every
-//     fragment, and widening those would be eight times the conversions.  They are fetched one tile earlier.
+//   * Values pass through registers on their way to LDS and are fp16 there, so that p goes to the second product as one fp16 number: as two bf16
+//     numbers beside bf16 values, twice the products, two chunks of 4680 rows took 938 us instead of 694, prompts 456 instead of 298 (one bf16
+//     number: 622 and 271, and 1.4 times the error).  e4m3 and most bf16 are exact in fp16; a tile that holds others is left out by the loop
+//     and taken afterwards as it is, which takes three to four times as long.
+//   * Keys of 8 bits are widened on the way too: every wave reads every fragment, and widening those would be eight times the
+//     conversions.  8-bit tiles are fetched one tile earlier.
 template <int NW>
 constexpr int kRowsStages = 65536 + (NW == 8 ? 8 * 8192 : 0);
 template <int NW>
@@ -617,7 +752,8 @@ constexpr int kRowsLds = kRowsStages<NW> + NW * kApartBytes + 64;      // bytes 
 
 template <bool E4M3, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows_kernel(PagedAttnArgs a) {
-    typedef Rows<false> R;                                    // in LDS keys and values are bf16 whatever the pages hold
+    typedef Rows<kFp16> R;                                    // values in LDS; keys are bf16 there whatever the pages hold
+    typedef Weights<kFp16> P;
     constexpr int KT = 64, kTile = KT * 256;
     constexpr int kRow = E4M3 ? 128 : 256;                    // bytes in a page
     constexpr int kLoads = KT * kRow / 1024 / NW;             // wave loads of a K or V tile by each wave
@@ -663,7 +799,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
         return;
     }
 
-    f32x16 o[4];
+    f32x16 o[4];                                              // (of bf16 pages: times kValueScale)
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -694,31 +830,50 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             }
             return s;
         };
-        // bf16: straight to LDS
+        // keys of bf16: straight to LDS
         const int k_lane = (lane >> 4) * 256 + (((lane & 15) ^ ((4 * wave + (lane >> 4)) & 15)) << 4);
-        const int v_lane = R::v_source(lane, 0);
-        auto fetch = [&](const void* pool, const Source& s, int lane_at, unsigned char* stage) {
+        auto fetch = [&](const Source& s, unsigned char* stage) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i)
-                load_to_lds(static_cast<const unsigned char*>(pool) + s.at[i] + lane_at, stage + 1024 * (wave + NW * i));
+                load_to_lds(static_cast<const unsigned char*>(a.k_pages) + s.at[i] + k_lane, stage + 1024 * (wave + NW * i));
         };
-        // e4m3: to registers, and from there as bf16
+        // values, and keys of e4m3: to registers, and from there in the format of LDS
         struct Bytes {
             uint4 x[kLoads];
         };
+        const int v_lane = E4M3 ? lane * 16 : R::v_source(lane, 0);
         auto take = [&](const void* pool, const Source& s) {
             Bytes b;
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) b.x[i] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(pool) + s.at[i] + lane * 16);
+            for (int i = 0; i < kLoads; ++i) b.x[i] = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(pool) + s.at[i] + v_lane);
             return b;
         };
-        auto put = [&](const Bytes& b, bool values, unsigned char* stage) {
+        auto put_keys = [&](const Bytes& b, unsigned char* stage) {
 #pragma unroll
             for (int i = 0; i < kLoads; ++i) {
-                const int row = 8 * (wave + NW * i) + (lane >> 3), c = 2 * (lane & 7), turn = values ? (row & 3) << 2 : row & 15;
+                const int row = 8 * (wave + NW * i) + (lane >> 3), c = 2 * (lane & 7), turn = row & 15;
                 *reinterpret_cast<bf16x8*>(stage + row * 256 + ((c ^ turn) << 4)) = widen_e4m3(u32x2{b.x[i].x, b.x[i].y});
                 *reinterpret_cast<bf16x8*>(stage + row * 256 + (((c + 1) ^ turn) << 4)) = widen_e4m3(u32x2{b.x[i].z, b.x[i].w});
             }
+        };
+        // and a word of this wave's for the tile: whether its values need care, because of their range or an infinity or NaN
+        auto put_values = [&](const Bytes& b, unsigned char* stage, unsigned* care_flags) {
+            bool care = false;
+            Range range;
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) {
+                if constexpr (E4M3) {
+                    const int row = 8 * (wave + NW * i) + (lane >> 3), c = 2 * (lane & 7);
+                    *reinterpret_cast<f16x8*>(stage + R::v_position(row, c)) = widen_to_fp16(u32x2{b.x[i].x, b.x[i].y});
+                    *reinterpret_cast<f16x8*>(stage + R::v_position(row, c + 1)) = widen_to_fp16(u32x2{b.x[i].z, b.x[i].w});
+                    care |= Rows<kE4m3>::broken(b.x[i]);
+                } else {
+                    *reinterpret_cast<f16x8*>(stage + 1024 * (wave + NW * i) + lane * 16) = scaled_to_fp16(b.x[i], range);
+                }
+            }
+            if (!E4M3) care = range.left();
+            const unsigned long long any = __builtin_amdgcn_ballot_w64(care);
+            if (lane == 0) care_flags[wave] = any != 0;
         };
 
         // ---- the wave's 32 rows, through LDS: eight waves behind the stages; four in the second stages, which are free until then
@@ -735,7 +890,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
         }
         hold_order();
         Source src0 = source_of(pages[0], first, 0), src1 = source_of(pages[1], first + 1, 1);
-        Source ahead;                                         // of the tile whose values are fetched next
+        Source ahead;                                         // e4m3: of the tile whose values are fetched next
         Bytes k_bytes, v_bytes, k_one;
         int next_pages;
         auto barrier = [&]() {
@@ -749,24 +904,26 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             v_bytes = take(a.v_pages, src0);
             k_one = take(a.k_pages, src1);
             const Bytes k_two = take(a.k_pages, src2), v_one = take(a.v_pages, src1);
-            put(k_bytes, false, k_stage);
-            put(v_bytes, true, v_stage);
-            if (NW == 8) put(k_one, false, k_stage + kTile);
+            put_keys(k_bytes, k_stage);
+            put_values(v_bytes, v_stage, flags);
+            if (NW == 8) put_keys(k_one, k_stage + kTile);
             k_bytes = k_two;
             v_bytes = v_one;
             ahead = src2;
             next_pages = pages[3];
             __builtin_amdgcn_s_waitcnt(0x0070);               // all loads, and what was put
         } else {
-            fetch(a.k_pages, src0, k_lane, k_stage);
+            fetch(src0, k_stage);
             hold_order();
-            fetch(a.v_pages, src0, v_lane, v_stage);
+            v_bytes = take(a.v_pages, src0);
             hold_order();
-            if (NW == 8) fetch(a.k_pages, src1, k_lane, k_stage + kTile);
+            if (NW == 8) fetch(src1, k_stage + kTile);
             hold_order();
-            ahead = src1;
+            const Bytes v_one = take(a.v_pages, src1);
+            put_values(v_bytes, v_stage, flags);
+            v_bytes = v_one;
             next_pages = pages[2];
-            __builtin_amdgcn_s_waitcnt(0x0F70 | ((NW == 8 ? 2 : 1) * kLoads));      // the rows and the first keys
+            __builtin_amdgcn_s_waitcnt(0x0070 | ((NW == 8 ? 2 : 1) * kLoads));      // the rows, the first keys, and what was put
         }
         barrier();
         bf16x8 qf[8];
@@ -775,10 +932,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
         if (NW == 4) {
             reads_done();
             barrier();                                        // everyone has its rows: the second stages are free
-            if constexpr (E4M3) put(k_one, false, k_stage + kTile);
-            else fetch(a.k_pages, src1, k_lane, k_stage + kTile);
+            if constexpr (E4M3) put_keys(k_one, k_stage + kTile);
+            else fetch(src1, k_stage + kTile);
         }
 
+        const int k_first = l31 * 256 + ((lh ^ (l31 & 15)) << 4);            // this lane's byte of step 0; of step s: 32 s turned into it
         // Half of S^T of the tile at sk: steps 4 half .. + 3 of both 32-key blocks, the fragments first, the products in turn to the two
         // accumulators (one that waits for its own predecessor takes 12 clocks longer).
         auto qk_half = [&](f32x16 (&s)[2], const unsigned char* sk, int half, auto&& after_reads) {
@@ -792,43 +950,37 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb)
-                    kf[i][kb] = *reinterpret_cast<const bf16x8*>(sk + (kb * 32 + l31) * 256 + (((2 * (4 * half + i) + lh) ^ (l31 & 15)) << 4));
+                for (int kb = 0; kb < 2; ++kb) kf[i][kb] = *reinterpret_cast<const bf16x8*>(sk + kb * 32 * 256 + (k_first ^ (32 * (4 * half + i))));
             after_reads();
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int kb = 0; kb < 2; ++kb) s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i][kb], qf[4 * half + i], s[kb], 0, 0, 0);
         };
-        auto nothing = []() {};
         int v_at[4];
 #pragma unroll
         for (int db = 0; db < 4; ++db) v_at[db] = R::v_lane(lane, db);
-
         const float scale = a.mask.scale_log2e;
+
+        int care_first = INT_MAX, care_last = -1;             // tiles whose values are left out by the loop (below)
+        auto nothing = []() {};
         f32x16 s_a[2], s_b[2];
         qk_half(s_a, k_stage, 0, nothing);
         qk_half(s_a, k_stage, 1, nothing);
 
         // One tile: s_cur holds S^T of tile n; S^T of tile n + 1 is formed into s_nxt on the way.  k_now: keys n + 1; k_fill: keys n + 2 go there;
         // v_now: values n; v_fill: values n + 1 go there (restrict: a transposing read is taken to wait for every load on its way to LDS
-        // that may alias it).  Past the last tile it is fetched again, unconditionally, into a stage that nobody reads.
+        // that may alias it); care_now, care_fill: the words of the values n and n + 1.  Past the last tile it is fetched again, unconditionally, into a stage that nobody reads.
         auto tile_step = [&](const unsigned char* __restrict__ k_now, unsigned char* __restrict__ k_fill, unsigned char* __restrict__ v_now,
-                             unsigned char* __restrict__ v_fill, f32x16 (&s_cur)[2], f32x16 (&s_nxt)[2], int n) __attribute__((always_inline)) {
-            if constexpr (E4M3) __builtin_amdgcn_s_waitcnt(0x0070);
-            else __builtin_amdgcn_s_waitcnt(0x0F70);
+                             unsigned char* __restrict__ v_fill, f32x16 (&s_cur)[2], f32x16 (&s_nxt)[2], int n, const unsigned* __restrict__ care_now,
+                             unsigned* __restrict__ care_fill) __attribute__((always_inline)) {
+            __builtin_amdgcn_s_waitcnt(0x0070);
             barrier();                       // keys n + 1 and values n are there; everyone is done with keys n and values n - 1
             const unsigned gaps = gaps_ahead & 15u;
             gaps_ahead >>= 4;
             const int key0 = key_of(n);
             const bool masked = gaps != 0 || !whole(vis, key0, key0 + KT);
             if (masked) {
-                // a share of the values each: infinities and NaN need care where a row does not see them (below)
-                bool hit = false;
-#pragma unroll
-                for (int i = 0; i < 16 / NW; ++i) hit |= R::broken(*reinterpret_cast<const uint4*>(v_now + (wave * (16 / NW) + i) * 1024 + lane * 16));
-                const unsigned long long hits = __builtin_amdgcn_ballot_w64(hit);
-                if (lane == 0) flags[wave] = hits != 0;
                 const RowKeys keys = row_keys(a.mask, place_of(own_row()).token, w.n, w.kv_len);
                 // bounds relative to this lane's first key; sixteen keys without a page are behind the end
                 const int mine = key0 + 4 * lh, before = keys.end - mine, from = keys.low - mine, sink = keys.sink - mine;
@@ -846,30 +998,30 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             }
             const Source src = source_of(next_pages, n + kAhead, kAhead - 1);
             float sums[4];
-            bf16x8 pf[4];
+            P pf[4];
             auto exps = [&](int kb) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(s_cur[kb][r], scale, -m));
                     sums[r & 3] = (kb == 0 && r < 4) ? p : sums[r & 3] + p;     // four independent chains
-                    pf[kb * 2 + (r >> 3)][r & 7] = (bf16)p;
+                    pf[kb * 2 + (r >> 3)].set(r & 7, p);
                 }
             };
             auto pin = [&]() {               // the fragments are formed here, among the products, not after the branch
 #pragma unroll
-                for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(pf[i]));
+                for (int i = 0; i < 4; ++i) pf[i].pin();
             };
+            if constexpr (E4M3) put_keys(k_bytes, k_fill);
+            put_values(v_bytes, v_fill, care_fill);
             if constexpr (E4M3) {
-                put(k_bytes, false, k_fill);
-                put(v_bytes, true, v_fill);
                 k_bytes = take(a.k_pages, src);
                 v_bytes = take(a.v_pages, ahead);
             }
             __builtin_amdgcn_sched_barrier(0);
             qk_half(s_nxt, k_now, 0, [&]() {
                 if constexpr (!E4M3) {
-                    fetch(a.k_pages, src, k_lane, k_fill);
-                    fetch(a.v_pages, ahead, v_lane, v_fill);
+                    fetch(src, k_fill);
+                    v_bytes = take(a.v_pages, src);
                 }
             });
             exps(0);
@@ -884,7 +1036,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             __builtin_amdgcn_sched_barrier(0);
             ahead = src;
             next_pages = look_up(n + kAhead + 1);
-            qk_half(s_nxt, k_now, 1, nothing);
+            bool care;                       // a wave's word of these values says so
+            qk_half(s_nxt, k_now, 1, [&]() { care = __builtin_amdgcn_ballot_w64(care_now[lane & (NW - 1)] != 0) != 0; });
             exps(1);
             float lsum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
             pin();
@@ -897,11 +1050,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             }
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(lsum <= kSumLimit)) != 0, 0)) {
-                // a row's scores have run ahead of its reference point (or it has seen no key yet): move it to their maximum
+                // a row's scores have run ahead of its reference point (or it has seen no key yet): move it to their maximum, which is more than
+                // log2(kSumLimit / 32) ahead
                 const float top = max2(block_max(s_cur[0]), block_max(s_cur[1])) * scale;
-                const bool moved = top > m + kSlack;
-                const float alpha = moved ? __builtin_amdgcn_exp2f(m - top) : 1.0f;
-                m = moved ? top : m;
+                const float next = top > m + (P::kLift + 1.0f) ? top - P::kLift : m, alpha = __builtin_amdgcn_exp2f(m - next);
+                m = next;
                 l *= alpha;
 #pragma unroll
                 for (int db = 0; db < 4; ++db)
@@ -914,31 +1067,18 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             }
             l += lsum;
             __builtin_amdgcn_sched_barrier(0);
-            if (masked) {
-                reads_done();
-                barrier();                   // what every wave saw of these values is written down
-                unsigned any = 0;
-#pragma unroll
-                for (int i = 0; i < NW; ++i) any |= flags[i];
-                if (__builtin_expect(__builtin_amdgcn_readfirstlane(any) != 0, 0)) {
-                    const unsigned broken0 = broken_keys<false>(v_now, 0, lane), broken1 = broken_keys<false>(v_now, 32, lane);
-                    unsigned char* const scratch = smem + kStages + wave * kApartBytes;
-                    add_apart<false>(o, v_now, 0, pf[0], pf[1], broken0, scratch, lane);
-                    add_apart<false>(o, v_now, 32, pf[2], pf[3], broken1, scratch, lane);
-                    reads_done();
-                    barrier();               // nobody needs them any more
-                    const unsigned long long all = broken0 | ((unsigned long long)broken1 << 32);
-                    for (int i = threadIdx.x; i < KT * 16; i += 64 * NW)
-                        if ((all >> (i >> 4)) & 1) *reinterpret_cast<uint4*>(v_now + i * 16) = uint4{0, 0, 0, 0};
-                    reads_done();
-                    barrier();
-                }
+            if (__builtin_expect(care, 0) && (!E4M3 || masked)) {        // (NaN that every row sees needs none)
+                care_first = min(care_first, n);
+                care_last = n;
+                return;
             }
 #pragma unroll
-            for (int ts = 0; ts < 4; ++ts)
+            for (int ts = 0; ts < 4; ++ts) {
+                typename R::Values v[4];
 #pragma unroll
-                for (int db = 0; db < 4; ++db)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(R::v_fragment(v_now + 16 * ts * 256, v_at[db]), pf[ts], o[db], 0, 0, 0);
+                for (int db = 0; db < 4; ++db) v[db] = R::v_fragment(v_now + 16 * ts * 256, v_at[db]);
+                add_values(o, v, pf[ts]);
+            }
             __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);       // fragment reads (two each) run four ahead of the products
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -948,15 +1088,84 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             __builtin_amdgcn_sched_barrier(0);
         };
         for (int n = first; n < end; n += 2) {
-            tile_step(k_stage + kTile, k_stage, v_stage, v_stage + kTile, s_a, s_b, n);
-            if (n + 1 < end) tile_step(k_stage, k_stage + kTile, v_stage + kTile, v_stage, s_b, s_a, n + 1);
+            tile_step(k_stage + kTile, k_stage, v_stage, v_stage + kTile, s_a, s_b, n, flags, flags + NW);
+            if (n + 1 < end) tile_step(k_stage, k_stage + kTile, v_stage + kTile, v_stage, s_b, s_a, n + 1, flags + NW, flags);
         }
         __builtin_amdgcn_s_waitcnt(0x0070);      // no load may still be on its way to this LDS when the wave ends
+
+        // ---- Tiles with values that do not go to the second product like others: bf16 beyond the range of fp16, which are taken as they are
+        // here, with p as two bf16 numbers; infinities and NaN in either format, which are added key by key.  Their p is in l already;
+        // their scores are formed once more, the same in the same order, and p at the last reference point.  Rare, so short, not fast.
+        for (int n = care_first; n <= care_last; ++n) {
+            constexpr int C = E4M3 ? kFp16 : kBf16;
+            const int key0 = key_of(n);
+            __syncthreads();                     // everyone is done with the stages
+            bool care = false;
+            for (int i = threadIdx.x; i < KT * kRow / 16; i += 64 * NW) {
+                const int r = i / (kRow / 16), c = i % (kRow / 16), key = key0 + r;
+                long long page = table[min(key >> a.batch.page_shift, a.batch.table_stride - 1)];
+                if ((unsigned long long)page >= (unsigned)a.batch.n_pages) page = 0;
+                const long long at = (((page * a.batch.kv_heads + w.hk) << a.batch.page_shift) + (key & slot_mask)) * kRow + c * 16;
+                const uint4 k = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(a.k_pages) + at);
+                const uint4 v = *reinterpret_cast<const uint4*>(static_cast<const unsigned char*>(a.v_pages) + at);
+                if constexpr (E4M3) {
+                    *reinterpret_cast<bf16x8*>(k_stage + r * 256 + (((2 * c) ^ (r & 15)) << 4)) = widen_e4m3(u32x2{k.x, k.y});
+                    *reinterpret_cast<bf16x8*>(k_stage + r * 256 + (((2 * c + 1) ^ (r & 15)) << 4)) = widen_e4m3(u32x2{k.z, k.w});
+                    *reinterpret_cast<f16x8*>(v_stage + R::v_position(r, 2 * c)) = widen_to_fp16(u32x2{v.x, v.y});
+                    *reinterpret_cast<f16x8*>(v_stage + R::v_position(r, 2 * c + 1)) = widen_to_fp16(u32x2{v.z, v.w});
+                    care |= Rows<kE4m3>::broken(v);
+                } else {
+                    Range range;
+                    scaled_to_fp16(v, range);
+                    care |= range.left();
+                    *reinterpret_cast<uint4*>(k_stage + r * 256 + ((c ^ (r & 15)) << 4)) = k;
+                    *reinterpret_cast<uint4*>(v_stage + R::v_position(r, c)) = v;
+                }
+            }
+            const unsigned long long cares = __builtin_amdgcn_ballot_w64(care);
+            if (lane == 0) flags[wave] = cares != 0;
+            const int page = look_up(n);
+            const unsigned gaps = (unsigned)__builtin_amdgcn_ballot_w64((unsigned)page >= (unsigned)a.batch.n_pages) & 15u;
+            __syncthreads();
+            // (the loop has taken those out of e4m3 of which every row sees every key in)
+            if (__builtin_amdgcn_ballot_w64(flags[lane & (NW - 1)] != 0) == 0 || (E4M3 && gaps == 0 && whole(vis, key0, key0 + KT))) continue;
+            qk_half(s_a, k_stage, 0, nothing);
+            qk_half(s_a, k_stage, 1, nothing);
+            const RowKeys keys = row_keys(a.mask, place_of(own_row()).token, w.n, w.kv_len);
+            auto seen = [&](int j) { return sees(keys, key0 + j) & (((gaps >> (j >> 4)) & 1) == 0); };
+            Weights<C> p[4];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int j = 8 * (i >> 2) + (i & 3) + 4 * lh;
+                const float x = seen(j) ? s_a[i >> 4][i & 15] : -INFINITY;
+                p[i >> 3].set(i & 7, __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -m)) * (E4M3 ? 1.0f : kValueScale));
+            }
+            unsigned broken[2];
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                broken[kb] = broken_keys<C>(v_stage, 32 * kb, lane);
+                add_apart<C>(o, v_stage, 32 * kb, p[2 * kb], p[2 * kb + 1], broken[kb], smem + kStages + wave * kApartBytes, lane,
+                             [&](int j) { return seen(32 * kb + j); });
+            }
+            __syncthreads();                     // nobody needs those any more
+            const unsigned long long all = broken[0] | ((unsigned long long)broken[1] << 32);
+            for (int i = threadIdx.x; i < KT * 16; i += 64 * NW)
+                if ((all >> (i >> 4)) & 1) *reinterpret_cast<uint4*>(v_stage + i * 16) = uint4{0, 0, 0, 0};
+            __syncthreads();
+#pragma unroll
+            for (int ts = 0; ts < 4; ++ts) {
+                typename Rows<C>::Values v[4];
+#pragma unroll
+                for (int db = 0; db < 4; ++db) v[db] = Rows<C>::v_fragment(v_stage + 16 * ts * 256, v_at[db]);
+                add_values(o, v, p[ts]);
+            }
+        }
     }
     const auto both = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
     const float total = __uint_as_float(both[0]) + __uint_as_float(both[1]);
     const Place x = place_of(own_row());
-    store_rows<4>(a, w, x.live, x.token, x.head, m, total, 0, lh == 0, lh, [&](int db, int g, int e) { return o[db][4 * g + e]; });
+    store_rows<4>(a, w, x.live, x.token, x.head, m, total, 0, lh == 0, lh,
+                  [&](int db, int g, int e) { return E4M3 ? o[db][4 * g + e] : o[db][4 * g + e] * (1.0f / kValueScale); });
 }
 
 }  // namespace

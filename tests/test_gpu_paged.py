@@ -415,6 +415,83 @@ def test_scores_far_below_zero(form):
     close(o, want, 2 * BF16 * want.abs())       # p to bf16, the result to bf16
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_weights_are_finer_than_the_output(form, e4m3):
+    """Two keys carry each row, with values of opposite sign: what remains of them is far smaller than either, so an error of p shows
+    where the output's own rounding does not cover it."""
+    q_len, kv_len = [300, 1, 40, 1], [128, 3, 700, 2000]
+    c = Cache(q_len, kv_len, 2, 16, e4m3, seed=7).fill(11)
+    for i, L in enumerate(kv_len):
+        pair = (0, L // 2)
+        for j in range(L):
+            page, slot = c.table[i, j // 16], j % 16
+            k = randn(31 * i + j, 2, D, dtype=torch.float32, scale=0.05)
+            k[:, :16] = 0.0 if j in pair else -13.0                # scores 73 and more below the pair's
+            c.k[page, :, slot] = (k / c.k_scale).to(c.k.dtype)
+        x = (randn(77 + i, 2, D, dtype=torch.float32) / c.v_scale).clamp(-448, 448).to(c.v.dtype).float()
+        for j, sign in zip(pair, (1.0, -1.0)):
+            c.v[c.table[i, j // 16], :, j % 16] = (sign * x).to(c.v.dtype)
+    q = randn(5, c.T, 8 * D)
+    q.view(c.T, 8, D)[:, :, :16] = 4.0
+    o = run_attention(c, q, 8, 0, 0, 0)
+    want, mass = attention_64(c, q, 8, 0, 0, 0)
+    # half a step of the output; p as two bf16 numbers (2^-16) or as one of fp16 (2^-11, and 2^-33 of the largest for each small one, of
+    # 2000 values up to 9); scores of 128 products in 32 bits, of size under 2^5 where they matter, move p by less than 2^-12
+    close(o, want, BF16 * want.abs() + (2.0 ** -12 + (2.0 ** -11 if e4m3 else 2.0 ** -16)) * mass + 2000 * 9 * 2.0 ** -33, "weights")
+
+
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+@pytest.mark.parametrize("low,high", [(-110, 80), (-30, -10), (0, 20)])
+def test_values_of_any_size(form, low, high):
+    """Channels of 2^low up to 2^high beside each other, some values far larger or smaller than their channel's others, and zeros."""
+    c = Cache([140, 1, 70], [500, 900, 70], 2, 16, seed=2, spare=0).fill(4)
+    r = np.random.RandomState(3)
+    size = torch.tensor(r.randint(low, high + 1, D)).double().exp2().cuda()
+    odd = randn(9, *c.v.shape, dtype=torch.float32)
+    v = c.v.double() * size
+    v = torch.where(odd > 3.3, v * 2.0 ** -9, torch.where(odd < -3.3, v * 2.0 ** 9, torch.where(odd.abs() < 0.01, 0.0, v)))
+    c.v.copy_(torch.where(c.v.isnan(), c.v.double(), v).to(torch.bfloat16))
+    q = randn(6, c.T, 8 * D)
+    for block, window in ((1, 0), (0, 0), (0, 200)):
+        o = run_attention(c, q, 8, block, window, 0)
+        want, mass = attention_64(c, q, 8, block, window, 0)
+        close(o, want, BF16 * want.abs() + 2.0 ** -10 * mass)      # p as fp16 (2^-11) or finer; scores move it by less than 2^-12
+
+
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+@pytest.mark.parametrize("size", [-26, -25, -23, 6, 7, 8])
+def test_values_at_the_ends_of_fp16(form, size):
+    """All of 2^size up to twice that, with zeros among them."""
+    c = Cache([140, 1], [500, 300], 1, 16, seed=2, spare=0).fill(4)
+    x = randn(8, *c.v.shape, dtype=torch.float32)
+    v = torch.copysign(1.0 + x.abs() % 1.0, x).to(torch.bfloat16).float().clamp(-1.9921875, 1.9921875) * 2.0 ** size
+    c.v.copy_(torch.where(c.v.isnan(), c.v, torch.where(x.abs() < 0.02, 0.0, v).to(torch.bfloat16)))
+    q = randn(6, c.T, 8 * D)
+    o = run_attention(c, q, 8, 1, 0, 0)
+    want, mass = attention_64(c, q, 8, 1, 0, 0)
+    close(o, want, BF16 * want.abs() + 2.0 ** -10 * mass)
+
+
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_infinite_values_that_every_row_sees(form):
+    """They come out as the formula has them: an infinity stays one, two of opposite sign and NaN are NaN; the other channels and the
+    other key head are as without them."""
+    c = Cache([140, 1], [500, 90], 2, 16, seed=2).fill(4)
+    q = randn(6, c.T, 8 * D)
+    clean, mass = attention_64(c, q, 8, 0, 0, 0)
+    inf = float("inf")
+    for j, channel, x in ((70, 3, inf), (200, 9, -inf), (71, 50, inf), (300, 50, -inf), (69, 127, float("nan"))):
+        c.v[c.table[0, j // 16], 1, j % 16, channel] = x
+    o = run_attention(c, q, 8, 0, 0, 0).double().cpu().view(c.T, 8, D)
+    hit = o[:140, 4:]
+    assert (hit[..., 3] == inf).all() and (hit[..., 9] == -inf).all() and hit[..., 50].isnan().all() and hit[..., 127].isnan().all()
+    rest = torch.ones(c.T, 8, D, dtype=torch.bool)
+    rest[:140, 4:, [3, 9, 50, 127]] = False
+    tol = BF16 * clean.abs() + (BF16 + 2.0 ** -12) * mass
+    close(o[rest], clean.view(c.T, 8, D)[rest], tol.view(c.T, 8, D)[rest], "what is not broken")
+
+
 def test_attention_offsets_beyond_32_bits():
     # a pool of 4.5 GiB, of which the last pages are used
     page, heads = 256, 8
