@@ -188,38 +188,12 @@ __device__ __forceinline__ bool locate(const PagedAttnArgs& a, int tile_rows, in
     if (w->seq >= a.batch.n_seqs) return false;
     w->q0 = s.q0;
     w->n = s.n;
-    w->kv_len = (int)min((long long)s.more, (long long)a.batch.table_stride << a.batch.page_shift);
+    w->kv_len = tokens_of(s.more, a.batch.table_stride, a.batch.page_shift);
     if (w->q0 < 0 || w->n < 0 || w->n > a.batch.n_tokens - w->q0) return false;      // not a batch: touch nothing
     w->rows = w->n * a.group;
     w->row0 = (tile - (int)((long long)w->q0 * a.group / tile_rows) - w->seq) * tile_rows;
     return w->row0 >= 0 && w->row0 < w->rows;
 }
-
-// The key tiles that a run of rows sees, in order: those of the sink, then those from the window on.
-struct Visited {
-    int sink_tiles, skip;     // tile number n is tile n where n < sink_tiles, n + skip from there on
-    int count;
-    int e_first, low_last, sink_first;      // which tiles need no mask: see whole()
-};
-template <int KT>
-__device__ __forceinline__ Visited visited_tiles(const MaskArgs& m, const Work& w, int first_token, int last_token) {
-    const RowKeys a = row_keys(m, first_token, w.n, w.kv_len), b = row_keys(m, last_token, w.n, w.kv_len);
-    Visited v;
-    v.e_first = a.end;
-    v.low_last = b.low;
-    v.sink_first = a.sink;
-    const int low_tile = a.low / KT, end_tile = (int)((unsigned)(b.end + KT - 1) / KT);
-    v.sink_tiles = (a.sink + KT - 1) / KT;
-    v.skip = v.sink_tiles < low_tile ? low_tile - v.sink_tiles : 0;
-    v.count = max(0, end_tile - v.skip);
-    return v;
-}
-__device__ __forceinline__ int tile_of(const Visited& v, int n) { return n < v.sink_tiles ? n : n + v.skip; }
-// Whether every row sees all keys first .. end - 1 (pages aside).
-__device__ __forceinline__ bool whole(const Visited& v, int first, int end) {
-    return end <= v.e_first && (first >= v.low_last || end <= v.sink_first);
-}
-__device__ __forceinline__ bool sees(const RowKeys& k, int j) { return (j < k.end) & ((j >= k.low) | (j < k.sink)); }
 
 // ---------------------------------------------------------------------------------------------------
 // Tiles of keys and values in LDS as they lie in a page, [key][128], a row's 16-byte chunks permuted so that fragment reads spread
@@ -454,7 +428,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
     w.part = (int)part;
     if (!locate(a, KT, (int)(rest - part * a.by_tiles.d), &w)) return;
     const int last_row = min(w.row0 + 32, w.rows) - 1;
-    const Visited vis = visited_tiles<KT>(a.mask, w, w.row0 / a.group, last_row / a.group);
+    const Visited vis = visited_tiles<KT>(a.mask, w.row0 / a.group, last_row / a.group, w.n, w.kv_len);
     const int first = min(vis.count, w.part * a.part_tiles), end = w.part == a.parts - 1 ? vis.count : min(vis.count, first + a.part_tiles);
     const int count = max(0, (end - first - wave + NW - 1) / NW);           // tiles of this wave
 
@@ -777,7 +751,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
     if (!locate(a, 32 * NW, a.row_tiles - 1 - (int)(logical - rest * a.by_tiles.d), &w)) return;
     const int last_row = min(w.row0 + 32 * NW, w.rows) - 1;
     const int first_token = (int)divide(w.row0, a.by_group), last_token = (int)divide(last_row, a.by_group);
-    const Visited vis = visited_tiles<KT>(a.mask, w, first_token, last_token);
+    const Visited vis = visited_tiles<KT>(a.mask, first_token, last_token, w.n, w.kv_len);
     const int first = min(vis.count, w.part * a.part_tiles), end = w.part == a.parts - 1 ? vis.count : min(vis.count, first + a.part_tiles);
     // this lane's row, formed anew where it is needed: kept across the loop it would be spilled
     auto own_row = [&]() {

@@ -2,6 +2,7 @@
 #pragma once
 
 #include "common.h"
+#include "paged_ranges.h"
 
 namespace sdv2 {
 
@@ -57,24 +58,6 @@ __device__ __forceinline__ Sequence sequence_at(const int* q_start, const int* m
     s.n = __builtin_amdgcn_readfirstlane(q_start[at + 1]) - s.q0;
     s.more = __builtin_amdgcn_readfirstlane(more[at]);
     return s;
-}
-
-// Keys that a row may see: j < end, and j >= low or j < sink.
-struct RowKeys {
-    int end, low, sink;
-};
-struct MaskArgs {
-    int block;                // 0: all keys; B: those of the row's block of B tokens and before
-    int window, sink;         // 0: no window; else the last `window` keys up to the end, and the first `sink`
-    float scale_log2e;        // softmax scale times log2 e (and the keys' scale)
-};
-// Row i of n new tokens of a sequence of kv_len tokens.
-__device__ __forceinline__ RowKeys row_keys(const MaskArgs& m, int i, int n, int kv_len) {
-    const int p = kv_len - n + i;
-    int end = max(kv_len, 0);
-    if (m.block > 0) end = p < 0 ? 0 : (int)min((long long)kv_len, ((long long)(p / m.block) + 1) * m.block);
-    const int low = m.window > 0 ? max(0, end - m.window) : 0;
-    return RowKeys{end, low, m.window > 0 ? min(m.sink, low) : 0};
 }
 
 // Eight bf16 from eight e4m3 (exact).

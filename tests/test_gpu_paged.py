@@ -564,6 +564,16 @@ def test_a_kv_len_beyond_the_table_counts_as_the_table():
     check_attention(c, randn(3, c.T, D), 1, 0, 0, 0)
 
 
+@pytest.mark.parametrize("block", [0, 1, 24])
+@pytest.mark.parametrize("kv_len", [-1, -(1 << 31), 3 - (1 << 31)])
+def test_a_negative_kv_len_is_no_token(kv_len, block):
+    c = Cache([5, 40, 2], [40, 64, 30], 2, 16).fill(1)
+    c.kv_len.copy_(ints([40, kv_len, 30]))
+    c.kv_len_list = [40, kv_len, 30]
+    o = check_attention(c, randn(2, c.T, 4 * D), 4, block, 0, 0)
+    assert (o[5:45] == 0).all()
+
+
 @pytest.mark.parametrize("starts", [[0, 9, 3, 12], [0, 3, 1 << 30, 12], [5, 2, -7, 12], [0, 3, 6, 400]])
 def test_rows_of_no_batch_touch_nothing_outside(starts):
     """Arrays that are no batch (they do not ascend, or leave the list): whatever rows come out, nothing outside is read or written."""

@@ -3,6 +3,8 @@ sizes they state.  The pointers of these calls are never read: each call ends be
 
 import ctypes as C
 import os
+import random
+import subprocess
 
 import pytest
 import torch
@@ -209,3 +211,73 @@ def test_tuning_refusals(lib, name, value):
     with pytest.raises(b.Sdv2Error) as e:
         b.tuning_set(name, value)
     assert e.value.code == INVALID
+
+
+@pytest.fixture(scope="module")
+def visits(tmp_path_factory):
+    """visits(kv_len, table_stride, page_shift, n, first, last, block, window, sink, tile) -> (tokens, [whole or masked tile, ...]) as the
+    kernels form them, compiled for the host."""
+    d = tmp_path_factory.mktemp("ranges")
+    (d / "ranges.cpp").write_text('''
+#include "paged_ranges.h"
+using namespace sdv2;
+template <int KT>
+static int run(const MaskArgs& m, int first, int last, int n, int tokens, int* out, int capacity) {
+    const Visited v = visited_tiles<KT>(m, first, last, n, tokens);
+    for (int i = 0; i < v.count && i < capacity; ++i) {
+        const int t = tile_of(v, i);
+        out[i] = 2 * t + (whole(v, t * KT, t * KT + KT) ? 1 : 0);
+    }
+    return v.count;
+}
+extern "C" int visits(int kv_len, int stride, int shift, int n, int first, int last, int block, int window, int sink, int tile, int* tokens, int* out, int capacity) {
+    const MaskArgs m{block, window, sink, 1.0f};
+    *tokens = tokens_of(kv_len, stride, shift);
+    return tile == 32 ? run<32>(m, first, last, n, *tokens, out, capacity) : run<64>(m, first, last, n, *tokens, out, capacity);
+}
+''')
+    csrc = os.path.join(os.path.dirname(b.LIB_PATH), "csrc")
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", csrc, str(d / "ranges.cpp"), "-o", str(d / "ranges.so")], check=True)
+    f = C.CDLL(str(d / "ranges.so")).visits
+    tokens, buf = C.c_int(), (C.c_int * 4096)()
+
+    def call(*args):
+        n = f(*args, C.byref(tokens), buf, 4096)
+        return tokens.value, n, [(x >> 1, bool(x & 1)) for x in buf[:max(0, min(n, 4096))]]
+    return call
+
+
+@pytest.mark.parametrize("block", [0, 1, 24, 2 ** 31 - 1])
+@pytest.mark.parametrize("window,sink", [(0, 0), (100, 30), (2 ** 31 - 1, 2 ** 31 - 1)])
+def test_lengths_of_no_sequence_visit_nothing_or_the_table(visits, block, window, sink):
+    """A kv_len of the device array that is no length, as far as 32 bits go, counts as none or as what the table holds."""
+    for kv_len in (-1, -5, -(2 ** 30), -(2 ** 31) + 1, -(2 ** 31)):
+        for n in (1, 7, 2 ** 20):
+            assert visits(kv_len, 4, 4, n, 0, n - 1, block, window, sink, 32) == (0, 0, [])
+            assert visits(kv_len, 2 ** 22, 8, n, 0, n - 1, block, window, sink, 64) == (0, 0, [])
+    for kv_len in (65, 2 ** 30, 2 ** 31 - 1):
+        tokens, count, tiles = visits(kv_len, 4, 4, 3, 0, 2, block, window, sink, 32)
+        assert tokens == 64 and 1 <= count <= 2 and tiles[-1][0] == 1
+    assert visits(2 ** 31 - 1, 2 ** 22, 8, 1, 0, 0, 1, 100, 0, 64)[:2] == (2 ** 30, 2)
+
+
+def test_visited_tiles_hold_every_key_that_is_seen(visits):
+    """Against the definition, key by key: every key that a row sees is in a visited tile, tiles ascend, and of a whole tile every row
+    sees every key."""
+    rng = random.Random(5)
+    for _ in range(1500):
+        n, kv_len = rng.randint(1, 90), rng.choice((0, 1, 31, 32, 33, rng.randint(0, 700)))
+        block, window, sink = rng.choice((0, 1, 3, 24, 100)), rng.choice((0, 0, 1, 17, 64, 200)), rng.choice((0, 1, 32, 40, 900))
+        first = rng.randrange(n)
+        last, tile = rng.randint(first, n - 1), rng.choice((32, 64))
+        _, count, tiles = visits(kv_len, 100, 4, n, first, last, block, window, sink, tile)
+        assert count == len(tiles) and [t for t, _ in tiles] == sorted({t for t, _ in tiles})
+        seen = []
+        for i in range(first, last + 1):
+            p = kv_len - n + i
+            end = kv_len if block == 0 else 0 if p < 0 else min(kv_len, (p // block + 1) * block)
+            seen.append({j for j in range(end) if window == 0 or j >= end - window or j < sink})
+        assert set().union(*seen) <= {j for t, _ in tiles for j in range(t * tile, t * tile + tile)}
+        for t, all_seen in tiles:
+            keys = set(range(t * tile, t * tile + tile))
+            assert not all_seen or all(keys <= s for s in seen)
