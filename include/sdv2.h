@@ -560,7 +560,7 @@ int32_t sdv2_attention_bf16(const void* q_dev, const void* const* k_dev, const v
  *   are device memory, read when the kernels run: a recorded graph follows what they hold at each replay.  Rows from
  *   q_start[n_seqs] up to n_tokens - 1 are padding: no output of theirs is written.  A table entry outside [0, n_pages) names no
  *   page (given back, or not there yet): what would be appended to it is dropped, and its keys are in nobody's sight.
- *   A kv_len above table_stride * page_tokens counts as that, one below zero as 0.  max_q_len and max_kv_len choose the form of a launch (and the
+ *   A kv_len above table_stride * page_tokens counts as that, one below zero as 0, in every call.  max_q_len and max_kv_len choose the form of a launch (and the
  *   workspace); longer sequences are served all the same, less evenly spread.
  * Pages: K and V each [n_pages][kv_heads][page_tokens][128], bf16, or e4m3 holding key / k_scale and value / v_scale.  A row of 128
  *   numbers is read as it lies, so that one appended token is 256 (128) bytes in a row per head.

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnArgs a, int waves_per_row
     if (PAGES) {
         const Sequence s = sequence_at(a.batch.q_start, a.batch.kv_len, a.batch.n_seqs, row, [](int end, int) { return end; });
         if (s.index >= a.batch.n_seqs) return;                 // behind the last sequence: nothing of it is written
-        const int at = s.more - s.n + row - s.q0;
+        const int at = tokens_of(s.more, a.batch.table_stride, a.batch.page_shift) - s.n + row - s.q0;      // (as the attention reads it)
         const int entry = at >> a.batch.page_shift;
         if (at >= 0 && entry < a.batch.table_stride) {
             const int page = a.batch.table[(long long)s.index * a.batch.table_stride + entry];

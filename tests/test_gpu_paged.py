@@ -564,6 +564,24 @@ def test_a_kv_len_beyond_the_table_counts_as_the_table():
     check_attention(c, randn(3, c.T, D), 1, 0, 0, 0)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("kv_len,rows", [(70, 10), (65, 2), (64 + 40, 100), (1 << 30, 5), ((1 << 31) - 1, 64)])
+def test_append_and_attention_agree_on_a_kv_len_beyond_the_table(kv_len, rows, e4m3):
+    """It counts as the table's 64 tokens for both: the new ones are the last of those, and each sees its own key."""
+    c = Cache([rows, 3], [64, 40], 2, 16, e4m3, extra_entries=0).fill(1)
+    c.kv_len.copy_(ints([kv_len, 40]))
+    c.batch = b.ragged_batch(c.q_start, c.kv_len, c.table_dev, c.T, rows, 64)
+    k, v = randn(2, c.T, 2 * D), randn(3, c.T, 2 * D)
+    b.paged_append(c.cfg, c.k, c.v, c.batch, k, v)
+    half, floor = (2.0 ** -4, 2.0 ** -10) if e4m3 else (0.0, 0.0)
+    for i in range(max(0, rows - 64), rows):
+        at = 64 - rows + i
+        for pages, x, scale in ((c.k, k, c.k_scale), (c.v, v, c.v_scale)):
+            want = (x[i].double().cpu() / scale).clamp(-448, 448).view(2, D)
+            close(pages[c.table[0, at // 16], :, at % 16].float(), want, (half * want.abs()).clamp(min=floor) + 4 * F32 * want.abs(), "token %d" % at)
+    check_attention(c, randn(4, c.T, 4 * D), 4, 1, 0, 0)
+
+
 @pytest.mark.parametrize("block", [0, 1, 24])
 @pytest.mark.parametrize("kv_len", [-1, -(1 << 31), 3 - (1 << 31)])
 def test_a_negative_kv_len_is_no_token(kv_len, block):
@@ -572,6 +590,9 @@ def test_a_negative_kv_len_is_no_token(kv_len, block):
     c.kv_len_list = [40, kv_len, 30]
     o = check_attention(c, randn(2, c.T, 4 * D), 4, block, 0, 0)
     assert (o[5:45] == 0).all()
+    before = c.k.clone()
+    b.paged_append(c.cfg, c.k, c.v, c.batch, randn(3, c.T, 2 * D), randn(4, c.T, 2 * D))
+    assert same_bits(before[c.table[1, :4]], c.k[c.table[1, :4]]) and not same_bits(before, c.k)
 
 
 @pytest.mark.parametrize("starts", [[0, 9, 3, 12], [0, 3, 1 << 30, 12], [5, 2, -7, 12], [0, 3, 6, 400]])
