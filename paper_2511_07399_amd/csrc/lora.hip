@@ -47,6 +47,12 @@ __device__ __forceinline__ float* u_row(const LoraArgs& a, int part, int row, in
     return a.u + ((long long)part * a.n_tokens + row) * a.u_ranks + rank;
 }
 
+// What of x is rounded to bf16 first: a number beyond the largest of bf16 would become an infinity.
+__device__ __forceinline__ float within_bf16(float x) {
+    constexpr float kLargest = 0x1.fep127f;
+    return __builtin_fabsf(x) < INFINITY ? __builtin_amdgcn_fmed3f(x, -kLargest, kLargest) : x;
+}
+
 constexpr int kDownWaves = 8;
 // bf16 numbers that one of u goes to the second product as: each takes off eight bits, and an output of 32 bits shows the 17th
 // (four frames of rank 64 against 64 bits: two pieces 1.9e-6 of the output, three 1.2e-7, which is the sum's own).
@@ -300,7 +306,7 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
                 float rest = now.u[k][e >> 2][e & 3];
 #pragma unroll
                 for (int h = 0; h < NP; ++h) {
-                    piece[h][e] = (bf16)rest;
+                    piece[h][e] = (bf16)(h == 0 ? within_bf16(rest) : rest);
                     const float less = rest - (float)piece[h][e];
                     rest = less == less ? less : 0.0f;         // (of an infinity nothing is left)
                 }

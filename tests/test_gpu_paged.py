@@ -684,6 +684,34 @@ def test_adapters_of_broken_rows(q_len, fp32):
     assert torch.equal(out.cpu()[whole], clean.cpu()[whole])
 
 
+def lora(x, a, w, scale, ids, q_len, y):
+    """(the call's result, the formula's in 64 bits)"""
+    starts, out = [0] + list(np.cumsum(q_len)), torch.empty_like(y)
+    ws = torch.empty(b.lora_workspace_bytes(len(q_len), x.shape[0], max(q_len), x.shape[1], a.shape[1]), dtype=torch.uint8, device="cuda")
+    b.lora_bf16(x, a, w, scale, ints(ids), ints(starts), max(q_len), y, out, ws)
+    want = y.double().cpu()
+    for i, idx in enumerate(ids):
+        rows, s = slice(starts[i], starts[i + 1]), 1.0 if scale is None else scale[idx].double().item()
+        want[rows] += (s * (x[rows].double().cpu() @ a[idx].double().cpu().t())) @ w[idx].double().cpu().t()
+    return out.double().cpu(), want
+
+
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("q_len", [[1, 1], [20, 9], [2100, 30]])
+def test_adapters_whose_u_is_beyond_bf16(q_len, fp32):
+    """u of 3.398e38: a number in 32 bits, but rounded to bf16 an infinity."""
+    K, N, T = 64, 64, sum(q_len)
+    x, a, w = (torch.zeros(*s, dtype=torch.bfloat16, device="cuda") for s in ((T, K), (2, 8, K), (2, N, 8)))
+    x[:, 0] = torch.finfo(torch.bfloat16).max
+    x[::2, 0] *= -1
+    a[:, 3, 0], w[:, :, 3] = 1.0, randn(3, 2, N, scale=0.2).clamp(-0.9, 0.9)
+    scale = torch.full((2,), 1.0025, device="cuda")
+    out, want = lora(x, a, w, scale, [0, 1], q_len, torch.zeros(T, N, dtype=torch.float32 if fp32 else torch.bfloat16, device="cuda"))
+    # u rounded to 32 bits (2^-24); as two bf16 numbers, the first the largest there is and the second, of what is left, 1/400 of u, up to
+    # 2^-8, or as three (2^-16 of 1/400); three products added up (3 roundings)
+    close(out, want, (2.0 ** -21 if fp32 else BF16 + 2.0 ** -15) * want.abs())
+
+
 @pytest.mark.parametrize("bound", [0, 1, 5])
 def test_adapters_of_sequences_longer_than_stated(bound):
     test_lora([40, 3, 0, 17], 320, 448, 24, 3, True, True, bound)
