@@ -14,6 +14,8 @@
 // (270 MB in 46 + 53 us, 2.7 TB/s); 1536 x 1536 45 -> 32; 32 bits, 5120 x 5120, 175 -> 119 (3.8 TB/s).
 #include "ragged.h"
 
+#include <type_traits>
+
 namespace sdv2 {
 
 namespace {
@@ -51,6 +53,13 @@ __device__ __forceinline__ float* u_row(const LoraArgs& a, int part, int row, in
 __device__ __forceinline__ float within_bf16(float x) {
     constexpr float kLargest = 0x1.fep127f;
     return __builtin_fabsf(x) < INFINITY ? __builtin_amdgcn_fmed3f(x, -kLargest, kLargest) : x;
+}
+
+// Zeros in the place of infinities and NaN.
+__device__ __forceinline__ bf16x8 numbers_of(bf16x8 x) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __builtin_fabsf((float)x[e]) < INFINITY ? x[e] : (bf16)0.0f;
+    return x;
 }
 
 constexpr int kDownWaves = 8;
@@ -201,8 +210,11 @@ __global__ __launch_bounds__(256) void lora_down_tile_kernel(LoraArgs a, unsigne
 // KS: steps of 32 ranks.  A wave has a block of 64 columns and the tile's tokens, sixteen at a time: the next sixteen's y and u are on
 // their way under this one's products.  Tokens are the rows of the result and lane l15 has columns 4 l15 .. + 3 (of four instructions),
 // so a token's y and out are sixteen lanes next to each other; B's rows, of one piece of memory, are turned into fragments through LDS.
+// Waves a SIMD: as many as the products and what is on its way need registers for.  The second pass over a group (below), which is
+// hardly ever made, would take one of them (rank 64, 8800 rows, 5120 x 5120: 103.6 us instead of 100.3).
+constexpr int lora_up_waves(int ks, int size) { return ks == 1 ? (size == 2 ? 5 : 4) : ks == 2 ? (size == 2 ? 4 : 3) : ks == 3 ? (size == 2 ? 3 : 2) : 2; }
 template <typename T, int KS, int TOKENS>
-__global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned groups) {
+__global__ __launch_bounds__(256, lora_up_waves(KS, sizeof(T))) void lora_up_kernel(LoraArgs a, unsigned groups) {
     typedef T four __attribute__((ext_vector_type(4)));
     __shared__ bf16x8 stage[4][64 * (4 * KS + 1)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -294,28 +306,45 @@ __global__ __launch_bounds__(256) void lora_up_kernel(LoraArgs a, unsigned group
         __builtin_amdgcn_sched_barrier(0);
         if (cut && 4 * (KS - 1) + lk >= pieces) now.u[KS - 1][0] = now.u[KS - 1][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         f32x4 acc[4];
+        auto multiply = [&](auto careful) {
+#pragma unroll
+            for (int m = 0; m < 4; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[m][e] = (float)now.v[e][m];
+#pragma unroll
+            for (int k = 0; k < KS; ++k) {
+                bf16x8 piece[NP];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float rest = now.u[k][e >> 2][e & 3];
+#pragma unroll
+                    for (int h = 0; h < NP; ++h) {
+                        piece[h][e] = (bf16)(h == 0 ? within_bf16(rest) : rest);
+                        const float less = rest - (float)piece[h][e];
+                        rest = less == less ? less : 0.0f;         // (of an infinity nothing is left)
+                    }
+                }
+#pragma unroll
+                for (int h = NP - 1; h >= 0; --h)
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        bf16x8 b = w[m][k];
+                        if (careful.value && h > 0) {
+                            asm volatile("" : "+v"(b));        // (here, not ahead of the loop)
+                            b = numbers_of(b);
+                        }
+                        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(piece[h], b, acc[m], 0, 0, 0);
+                    }
+            }
+        };
+        multiply(std::false_type());
+        float broken = 0.0f;
 #pragma unroll
         for (int m = 0; m < 4; ++m)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[m][e] = (float)now.v[e][m];
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            bf16x8 piece[NP];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float rest = now.u[k][e >> 2][e & 3];
-#pragma unroll
-                for (int h = 0; h < NP; ++h) {
-                    piece[h][e] = (bf16)(h == 0 ? within_bf16(rest) : rest);
-                    const float less = rest - (float)piece[h][e];
-                    rest = less == less ? less : 0.0f;         // (of an infinity nothing is left)
-                }
-            }
-#pragma unroll
-            for (int h = NP - 1; h >= 0; --h)
-#pragma unroll
-                for (int m = 0; m < 4; ++m) acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(piece[h], w[m][k], acc[m], 0, 0, 0);
-        }
+            for (int e = 0; e < 4; ++e) broken = __builtin_fmaf(acc[m][e], 0.0f, broken);
+        // an infinity in B times a second piece of u, which may be zero or of the other sign, is in none of the sums of the formula
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(broken == 0.0f)) != 0, 0)) multiply(std::true_type());
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             four v;

@@ -712,6 +712,28 @@ def test_adapters_whose_u_is_beyond_bf16(q_len, fp32):
     close(out, want, (2.0 ** -21 if fp32 else BF16 + 2.0 ** -15) * want.abs())
 
 
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("q_len", [[1, 1], [20, 9], [2100, 30]])
+def test_adapters_with_infinities_in_b(q_len, fp32):
+    """They come out as the formula has them, in their own columns: a second piece of u is zero, or of the other sign."""
+    K, N, rank, T = 128, 192, 24, sum(q_len)
+    x, a, w = randn(1, T, K), randn(2, 2, rank, K, scale=0.1), randn(3, 2, N, rank, scale=0.3)
+    x[0] = 0.0                                  # u = 0: zero times infinity is NaN
+    a[0, 5] = 0.0
+    a[0, 5, 7] = 1.0                            # u[5] is a bf16 number, of which nothing is left for the second piece
+    y = randn(5, T, N, dtype=torch.float32 if fp32 else torch.bfloat16)
+    clean, _ = lora(x, a, w, None, [0, 1], q_len, y)
+    inf = float("inf")
+    for i, column, r, value in ((0, 3, 5, inf), (0, 64, 5, -inf), (1, 70, 0, inf), (1, 71, 23, -inf), (0, 130, 8, inf), (0, 130, 9, inf),
+                                (1, 191, 4, float("nan"))):
+        w[i, column, r] = value
+    out, want = lora(x, a, w, None, [0, 1], q_len, y)
+    broken = ~torch.isfinite(want)
+    assert broken[:, [3, 64, 130]][:q_len[0]].all() and broken[:, [70, 71, 191]][q_len[0]:].all()
+    assert torch.equal(out.isnan(), want.isnan()) and torch.equal(out[broken & ~want.isnan()], want[broken & ~want.isnan()])
+    assert torch.equal(out[~broken], clean[~broken])
+
+
 @pytest.mark.parametrize("bound", [0, 1, 5])
 def test_adapters_of_sequences_longer_than_stated(bound):
     test_lora([40, 3, 0, 17], 320, 448, 24, 3, True, True, bound)
