@@ -734,6 +734,23 @@ def test_adapters_with_infinities_in_b(q_len, fp32):
     assert torch.equal(out[~broken], clean[~broken])
 
 
+@pytest.mark.parametrize("q_len", [[1, 1], [20, 9], [2100, 30]])
+def test_adapters_of_fp32_rows_have_all_bits_of_u(q_len):
+    """u is one product, exact but for the scale, so all that is lost is lost behind it."""
+    K, N, rank, T = 64, 128, 8, sum(q_len)
+    x, a, w = torch.zeros(T, K, dtype=torch.bfloat16, device="cuda"), randn(2, 2, rank, K), randn(3, 2, N, rank)
+    x[torch.arange(T), torch.arange(T) % K] = randn(1, T)
+    scale = torch.tensor([0.7, 1.3], device="cuda")
+    y = torch.zeros(T, N, device="cuda")
+    out, want = lora(x, a, w, scale, [0, 1], q_len, y)
+    starts, mass = [0, q_len[0], T], torch.zeros_like(want)
+    for i in range(2):
+        rows = slice(starts[i], starts[i + 1])
+        mass[rows] = scale[i].item() * (x[rows].double().cpu() @ a[i].double().cpu().t()).abs() @ w[i].double().cpu().abs().t()
+    # scaled to 32 bits (2^-24), cut into three pieces of eight bits (2^-24), three times eight products added up (24 roundings)
+    close(out, want, 26 * F32 * mass)
+
+
 @pytest.mark.parametrize("bound", [0, 1, 5])
 def test_adapters_of_sequences_longer_than_stated(bound):
     test_lora([40, 3, 0, 17], 320, 448, 24, 3, True, True, bound)
