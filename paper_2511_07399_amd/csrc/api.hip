@@ -2228,18 +2228,6 @@ int32_t sdv2_paged_append(const sdv2_paged_cfg* cfg, void* k_pages_dev, void* v_
     return SDV2_OK;
 }
 
-static const char* paged_attention_wrong(const sdv2_paged_cfg* cfg, const sdv2_ragged_batch* batch, const sdv2_attn_mask* mask, int32_t q_heads) {
-    if (const char* why = paged_cfg_wrong(cfg)) return why;
-    if (const char* why = batch_wrong(batch, cfg)) return why;
-    if (!mask || mask->struct_size != sizeof(sdv2_attn_mask)) return "mask is null or its struct_size wrong";
-    if (mask->block < 0 || mask->window < 0 || mask->sink < 0) return "negative block, window or sink";
-    if (mask->scale != mask->scale || isinf(mask->scale)) return "scale is not finite";
-    if (q_heads <= 0 || q_heads % cfg->kv_heads) return "q_heads must be a multiple of kv_heads";
-    if ((int64_t)batch->n_tokens * q_heads > kMostRowHeads) return "more than 2^26 heads of rows";
-    if ((int64_t)batch->n_seqs * cfg->kv_heads > ((int64_t)1 << 21)) return "more than 2^21 key heads of sequences";
-    return nullptr;
-}
-
 static MaskArgs mask_args(const sdv2_attn_mask* m, const sdv2_paged_cfg* cfg) {
     MaskArgs a{};
     a.block = m->block;
@@ -2248,6 +2236,21 @@ static MaskArgs mask_args(const sdv2_attn_mask* m, const sdv2_paged_cfg* cfg) {
     const float scale = m->scale > 0.0f ? m->scale : 1.0f / sqrtf((float)SDV2_HEAD_DIM);
     a.scale_log2e = scale * 1.4426950408889634f * cfg->k_scale;
     return a;
+}
+
+static const char* paged_attention_wrong(const sdv2_paged_cfg* cfg, const sdv2_ragged_batch* batch, const sdv2_attn_mask* mask, int32_t q_heads) {
+    if (const char* why = paged_cfg_wrong(cfg)) return why;
+    if (const char* why = batch_wrong(batch, cfg)) return why;
+    if (!mask || mask->struct_size != sizeof(sdv2_attn_mask)) return "mask is null or its struct_size wrong";
+    if (mask->block < 0 || mask->window < 0 || mask->sink < 0) return "negative block, window or sink";
+    if (mask->scale != mask->scale || isinf(mask->scale)) return "scale is not finite";
+    // (a masked score is minus infinity: times zero it would be NaN, as would a score of zero times an infinity)
+    const float scale = mask_args(mask, cfg).scale_log2e;
+    if (scale == 0.0f || isinf(scale)) return "scale times k_scale is zero or infinite in 32 bits";
+    if (q_heads <= 0 || q_heads % cfg->kv_heads) return "q_heads must be a multiple of kv_heads";
+    if ((int64_t)batch->n_tokens * q_heads > kMostRowHeads) return "more than 2^26 heads of rows";
+    if ((int64_t)batch->n_seqs * cfg->kv_heads > ((int64_t)1 << 21)) return "more than 2^21 key heads of sequences";
+    return nullptr;
 }
 
 static size_t paged_attention_bytes(const PagedAttnPlan& plan, int64_t row_heads) {

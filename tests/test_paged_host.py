@@ -129,6 +129,21 @@ def test_mask_refusals(lib, bad):
     assert attend(lib, cfg(), batch(), None) == INVALID
 
 
+@pytest.mark.parametrize("scale,k_scale", [(1e-20, 1e-30), (1e-30, 1e-20), (1e20, 1e30), (3e38, 1.0)])
+def test_a_scale_of_zero_or_infinity_with_the_keys_scale_is_refused(lib, scale, k_scale):
+    """Times the keys' scale it multiplies masked scores, minus infinity: zero would make them NaN."""
+    c = cfg(k_scale=k_scale) if k_scale == 1.0 else cfg(format=1, k_scale=k_scale)
+    assert attend(lib, c, batch(), mask(scale=scale)) == INVALID
+    assert lib.sdv2_paged_attention_workspace_bytes(ref(c), ref(batch(n_tokens=1, max_kv_len=60000)), ref(mask(scale=scale)), 4) == 0
+
+
+@pytest.mark.parametrize("scale,k_scale", [(0.0, 1e-30), (0.0, 1e30), (1e-37, 1.0), (1e-39, 1.0), (1e8, 1e30), (-1.0, 0.5), (2e38, 1.0)])
+def test_scales_at_the_ends_are_taken(lib, scale, k_scale):
+    empty = batch(n_tokens=0, max_q_len=0)
+    c = cfg(k_scale=k_scale) if k_scale == 1.0 else cfg(format=1, k_scale=k_scale)
+    assert attend(lib, c, empty, mask(scale=scale)) == OK
+
+
 def test_attention_workspace_is_checked(lib):
     long = batch(n_seqs=1, n_tokens=1, max_q_len=1, max_kv_len=60000, table_stride=4000)
     need = lib.sdv2_paged_attention_workspace_bytes(ref(cfg()), ref(long), ref(mask()), 4)
