@@ -14,7 +14,6 @@
 #include "ragged.h"
 
 #include <climits>
-#include <mutex>
 #include <type_traits>
 
 namespace sdv2 {
@@ -411,7 +410,7 @@ __global__ __launch_bounds__(256, 2) void paged_attention_tokens_kernel(PagedAtt
     constexpr int kStages = E4M3 ? 2 : 1;
     constexpr int kTile = KT * R::kRow, kLoads = KT / R::kPerLoad;          // bytes and wave loads of a K or V tile
     static_assert(NW * kStages * 2 * kTile == kTokenStages, "and the waves' outputs fill it too");
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kTokenLds];      // (its size stated here, a launch sets no attribute: it may be the first, and recorded)
     unsigned char* const k_first = smem;
     unsigned char* const v_first = smem + NW * kTile;
     unsigned char* const k_second = smem + 2 * NW * kTile;
@@ -733,7 +732,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
     constexpr int kLoads = KT * kRow / 1024 / NW;             // wave loads of a K or V tile by each wave
     constexpr int kLoadRows = 1024 / kRow;
     constexpr int kAhead = E4M3 ? 3 : 2;                      // tiles between the fetch of keys and their softmax
-    extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[kRowsLds<NW>];
     unsigned char* const k_stage = smem;                      // [2][64 keys][256 B]
     unsigned char* const v_stage = smem + 2 * kTile;          // [2][64 keys][256 B]
     constexpr int kStages = kRowsStages<NW>;                  // behind them eight waves' rows, then add_apart's scratch and a word per wave
@@ -1230,16 +1229,6 @@ PagedAttnPlan plan_paged_attention(const RaggedArgs& b, const MaskArgs& mask, in
 
 hipError_t launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan& plan, int e4m3, hipStream_t s) {
     typedef void (*Kernel)(PagedAttnArgs);
-    static std::once_flag attr_once;
-    static hipError_t attr_err = hipSuccess;
-    std::call_once(attr_once, [&]() {
-        const std::pair<Kernel, int> kernels[] = {{paged_attention_tokens_kernel<false>, kTokenLds}, {paged_attention_tokens_kernel<true>, kTokenLds},
-                                                  {paged_attention_rows_kernel<false, 4>, kRowsLds<4>}, {paged_attention_rows_kernel<true, 4>, kRowsLds<4>},
-                                                  {paged_attention_rows_kernel<false, 8>, kRowsLds<8>}, {paged_attention_rows_kernel<true, 8>, kRowsLds<8>}};
-        for (const auto& k : kernels)
-            if (attr_err == hipSuccess) attr_err = hipFuncSetAttribute(reinterpret_cast<const void*>(k.first), hipFuncAttributeMaxDynamicSharedMemorySize, k.second);
-    });
-    if (attr_err != hipSuccess) return attr_err;
     PagedAttnArgs a = args;
     a.parts = plan.parts;
     a.part_tiles = plan.part_tiles;
@@ -1249,10 +1238,10 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, const PagedAttnPlan
     a.by_tiles = fast_div((unsigned)a.row_tiles, (unsigned long long)n_wg);
     a.by_heads = fast_div((unsigned)a.batch.kv_heads, (unsigned long long)n_wg);
     a.by_group = fast_div((unsigned)a.group, (unsigned long long)a.batch.n_tokens * a.group);
-    auto go = [&](Kernel k, int threads, int lds) { hipLaunchKernelGGL(k, dim3(a.n_wg), dim3(threads), lds, s, a); };
-    if (plan.rows == 32) go(e4m3 ? paged_attention_tokens_kernel<true> : paged_attention_tokens_kernel<false>, 256, kTokenLds);
-    else if (plan.rows == 128) go(e4m3 ? paged_attention_rows_kernel<true, 4> : paged_attention_rows_kernel<false, 4>, 256, kRowsLds<4>);
-    else go(e4m3 ? paged_attention_rows_kernel<true, 8> : paged_attention_rows_kernel<false, 8>, 512, kRowsLds<8>);
+    auto go = [&](Kernel k, int threads) { hipLaunchKernelGGL(k, dim3(a.n_wg), dim3(threads), 0, s, a); };
+    if (plan.rows == 32) go(e4m3 ? paged_attention_tokens_kernel<true> : paged_attention_tokens_kernel<false>, 256);
+    else if (plan.rows == 128) go(e4m3 ? paged_attention_rows_kernel<true, 4> : paged_attention_rows_kernel<false, 4>, 256);
+    else go(e4m3 ? paged_attention_rows_kernel<true, 8> : paged_attention_rows_kernel<false, 8>, 512);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && plan.parts > 1) {
         const long long row_heads = (long long)a.batch.n_tokens * a.q_heads;

@@ -2,6 +2,9 @@
 implementation in 64 bits, and together as an attention layer uses them."""
 
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -899,6 +902,42 @@ def test_a_recorded_layer_follows_lengths_and_tables():
         for st, w in zip((s, s2), want):
             assert same_bits(st["x"], w[0]) and same_bits(st["q"][:3], w[1]) and same_bits(st["o"][:3], w[2])
         assert same_bits(c.k, k1) and same_bits(c.v, v1)
+
+
+FIRST_CALLS = """
+import sys
+sys.path.insert(0, {tests!r}), sys.path.insert(0, {root!r})
+import torch
+import test_gpu_paged as t
+c = t.Cache([1, 30, 200], [900, 400, 200], 2, 32, {e4m3}).fill(1)
+q = t.randn(2, c.T, 16 * t.D)
+outs, graphs = [torch.zeros_like(q) for _ in range(3)], []
+for rows, o in zip((32, 128, 256), outs):
+    t.b.tuning_set("paged_rows", rows)
+    need = t.b.paged_attention_workspace_bytes(c.cfg, c.batch, t.b.attn_mask(1), 16)
+    ws = torch.empty(need + 16, dtype=torch.uint8, device="cuda")
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        t.b.paged_attention(c.cfg, c.k, c.v, c.batch, t.b.attn_mask(1), q, o, ws)
+    graphs.append((g, ws))
+for _ in range(3):
+    for o in outs:
+        o.zero_()
+    for g, _ in graphs:
+        g.replay()
+    torch.cuda.synchronize()
+    for rows, o in zip((32, 128, 256), outs):
+        t.b.tuning_set("paged_rows", rows)
+        assert torch.equal(o, t.run_attention(c, q, 16, 1, 0, 0)), rows
+print("same")
+"""
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+def test_the_first_calls_of_a_program_may_be_recorded(e4m3):
+    here = os.path.dirname(os.path.abspath(__file__))
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(tests=here, root=os.path.dirname(here), e4m3=e4m3)], capture_output=True, text=True, timeout=100)
+    assert r.returncode == 0 and r.stdout.strip().endswith("same"), r.stderr[-2000:]
 
 
 def test_the_same_call_twice_has_the_same_bits():

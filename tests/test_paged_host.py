@@ -296,3 +296,12 @@ def test_visited_tiles_hold_every_key_that_is_seen(visits):
         for t, all_seen in tiles:
             keys = set(range(t * tile, t * tile + tile))
             assert not all_seen or all(keys <= s for s in seen)
+
+
+def test_launches_of_paged_attention_set_no_attribute(lib):
+    """Its kernels state their LDS themselves, so a launch asks for none, and may be a program's first and recorded into a graph."""
+    from test_library_host import kernel_metadata
+    found = [(n, k) for n, k in kernel_metadata().items() if "paged_attention_tokens_kernel" in n or "paged_attention_rows_kernel" in n]
+    assert len(found) == 6
+    for name, k in found:
+        assert 65536 < k[".group_segment_fixed_size"] <= 163840, name
