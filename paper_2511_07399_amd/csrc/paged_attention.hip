@@ -920,10 +920,12 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
                     for (int r = 0; r < 16; ++r) s[kb][r] = 0.0f;
             }
             bf16x8 kf[4][2];
+            int at = k_first;
+            if (NW == 4) asm volatile("" : "+v"(at));         // (its eight places, kept across the loop, would cost the queries their registers)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int kb = 0; kb < 2; ++kb) kf[i][kb] = *reinterpret_cast<const bf16x8*>(sk + kb * 32 * 256 + (k_first ^ (32 * (4 * half + i))));
+                for (int kb = 0; kb < 2; ++kb) kf[i][kb] = *reinterpret_cast<const bf16x8*>(sk + kb * 32 * 256 + (at ^ (32 * (4 * half + i))));
             after_reads();
 #pragma unroll
             for (int i = 0; i < 4; ++i)
