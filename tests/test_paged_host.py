@@ -305,3 +305,12 @@ def test_launches_of_paged_attention_set_no_attribute(lib):
     assert len(found) == 6
     for name, k in found:
         assert 65536 < k[".group_segment_fixed_size"] <= 163840, name
+
+
+def test_paged_attention_kernels_spill_nothing(lib):
+    """A spilled register is reloaded from memory, and the wait for it is a wait for every tile load in flight."""
+    from test_library_host import kernel_metadata
+    found = [(n, k) for n, k in kernel_metadata().items() if "paged_attention" in n]
+    assert len(found) == 9
+    for name, k in found:
+        assert k[".vgpr_spill_count"] == 0 and k[".private_segment_fixed_size"] == 0, (name, k[".vgpr_spill_count"])
