@@ -2313,8 +2313,8 @@ static const char* lora_wrong(const sdv2_lora_cfg* c) {
     return nullptr;
 }
 
-// sixteens of tokens of one sequence each, as the kernels number them; none where every sequence has one token at most
-static int lora_slots(const sdv2_lora_cfg* c) { return c->n_tokens > 0 && c->max_q_len > 1 ? c->n_tokens / 16 + c->n_seqs : 0; }
+// sixteens of tokens of one sequence each, as the kernels number them; none where u has a row for each token
+static int lora_slots(const sdv2_lora_cfg* c) { return c->n_tokens > 0 && !lora_by_tokens(c->max_q_len) ? c->n_tokens / 16 + c->n_seqs : 0; }
 static size_t lora_bytes(const sdv2_lora_cfg* c, int parts) {
     const size_t rows = lora_slots(c) ? (size_t)lora_slots(c) * 16 : c->n_tokens;
     return align_up(parts * rows * align_up(c->rank, 16) * sizeof(float), 256);

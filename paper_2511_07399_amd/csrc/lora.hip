@@ -8,7 +8,7 @@
 //     eight waves in turn over pieces of 64 of K, K in parts over workgroups.  Many: lora_down_tile_kernel, 32 tokens.  u stays in 32
 //     bits, and goes to the second product as two or three bf16 numbers that add up to it (kPieces: as one, its rounding would be the
 //     result's largest error).
-//   out: lora_up_kernel, tokens as rows, y as the accumulator's start; one token a sequence: lora_up_few_kernel, on the vector unit.
+//   out: lora_up_kernel, tokens as rows, y as the accumulator's start; one or two tokens a sequence: lora_up_few_kernel, on the vector unit.
 // What the cache is asked for a load decides: 16 bytes of a lane are an access by themselves unless the lanes next to it are in the same
 // line.  8800 tokens of four sequences, bf16, 5120 x 5120 of rank 64: fragments straight from memory 145 us, rows by lines through LDS 97
 // (270 MB in 46 + 53 us, 2.7 TB/s); 1536 x 1536 45 -> 32; 32 bits, 5120 x 5120, 175 -> 119 (3.8 TB/s).
@@ -355,7 +355,7 @@ __global__ __launch_bounds__(256, lora_up_waves(KS, sizeof(T))) void lora_up_ker
     }
 }
 
-// One token of a sequence: on the vector unit, where a tile would be empty but for one of sixteen tokens.  B's rows lie one behind the
+// One or two tokens of a sequence: on the vector unit, where a tile would be empty but for those of sixteen tokens.  B's rows lie one behind the
 // other, so lanes next to each other read pieces of eight ranks next to each other: P lanes have a column (P the power of two from the
 // pieces of a row on), 64 / P columns a load, and add up by moves within the row of lanes; of the P loads that cover 64 columns a lane
 // keeps the sum of one, its own.  B's bytes bound it: 64 tokens of 16 adapters beside 5120 x 15 360, both launches, rank 16 15.2 us, 64
@@ -434,12 +434,12 @@ __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned g
     }
 }
 
-// Tiles of sixteen tokens and ranks, K in parts, for one token a sequence and wherever that is under half a workgroup a compute unit; else
+// Tiles of sixteen tokens and ranks, K in parts, for one or two tokens a sequence and wherever that is under half a workgroup a compute unit; else
 // tiles of 32 tokens by lines.  Measured, by sixteens | by 32 in us, 5120 x 5120: 16 sequences of 4 tokens of rank 16 10.0 | 13.5, of 48
 // 13.9 | 19.5; one of 1000 of rank 128 38.7 | 32.6; 128 of 16 of rank 16 30.2 | 25.6; 1536 x 4608: 100 of 4 14.7 | 15.5, of 16 17.5 | 17.4,
 // 64 of 24 of rank 64 26.0 | 23.1, 64 of 16 19.6 | 20.1.
 int sixteens(int n_seqs, int n_tokens, int rank) { return max(n_tokens / 16, n_seqs) * ((rank + 15) / 16); }
-bool by_sixteens(int n_seqs, int n_tokens, int max_q_len, int rank) { return max_q_len <= 1 || sixteens(n_seqs, n_tokens, rank) < kUnits / 2; }
+bool by_sixteens(int n_seqs, int n_tokens, int max_q_len, int rank) { return lora_by_tokens(max_q_len) || sixteens(n_seqs, n_tokens, rank) < kUnits / 2; }
 
 template <typename T, int TOKENS>
 void launch_up_tiles(const LoraArgs& a, hipStream_t s) {
@@ -454,9 +454,7 @@ void launch_up_tiles(const LoraArgs& a, hipStream_t s) {
 }
 template <typename T>
 void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
-    // (by lanes | by tiles: 64 sequences of one token 15.2 | 18.4 us, of two 14.9 | 16.3; 16 of one, 5120 x 5120, 9.1 | 9.2, of two 9.6 | 9.3,
-    // of four 11.6 | 9.5)
-    if (max_q_len <= 1) {
+    if (lora_by_tokens(max_q_len)) {
         auto go = [&](auto kernel, int blocks) {
             const unsigned groups = (unsigned)(a.N / 64 + 4 * blocks - 1) / (4 * blocks);
             hipLaunchKernelGGL(kernel, dim3(groups * (unsigned)(a.n_tokens / 16 + a.n_seqs)), dim3(256), 0, s, a, groups);
@@ -472,6 +470,11 @@ void launch_up(const LoraArgs& a, int max_q_len, hipStream_t s) {
     else launch_up_tiles<T, 32>(a, s);
 }
 }  // namespace
+
+// By lanes | by tiles, both launches, us: 64 sequences of one token, 5120 to 15 360, rank 16, 15.1 | 20.7, of two 18.6 | 21.7, of four 25.1 | 23.6;
+// of rank 64 one 30.9 | 39.9, two 34.9 | 39.8; of rank 128 two 58.9 | 67.9; 16, 5120 x 5120, rank 16, one 8.9 | 9.7, two 9.6 | 9.9, four 11.5 | 10.2;
+// 8 of three 10.7 | 9.7; 1000 of two, 1536 x 1536, rank 16, 25.9 | 31.2, 5120 x 5120, rank 128, 371 | 310.
+bool lora_by_tokens(int max_q_len) { return max_q_len <= 2; }
 
 int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank) {
     if (!by_sixteens(n_seqs, n_tokens, max_q_len, rank)) return 1;

@@ -137,6 +137,8 @@ struct LoraArgs {
     int parts;
     int slots;                        // sixteens of tokens of one sequence each; 0: u is [parts][n_tokens][u_ranks]
 };
+// whether the second product takes a sequence's tokens one by one, and u has a row for each (slots = 0)
+bool lora_by_tokens(int max_q_len);
 // parts of K: n_seqs, n_tokens, max_q_len, K, rank
 int lora_parts(int n_seqs, int n_tokens, int max_q_len, int K, int rank);
 hipError_t launch_lora(const LoraArgs& a, int max_q_len, hipStream_t s);

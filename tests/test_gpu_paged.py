@@ -754,6 +754,13 @@ def test_adapters_of_fp32_rows_have_all_bits_of_u(q_len):
     close(out, want, 26 * F32 * mass)
 
 
+@pytest.mark.parametrize("fp32", [False, True])
+@pytest.mark.parametrize("rank", [8, 40, 128])
+def test_adapters_of_two_tokens(rank, fp32):
+    test_lora([2, 1, 0, 2] * 9, 2048, 832, rank, 3, fp32, not fp32)
+    test_lora([17, 2, 40], 128, 64, rank, 2, fp32, True, 2)
+
+
 @pytest.mark.parametrize("bound", [0, 1, 5])
 def test_adapters_of_sequences_longer_than_stated(bound):
     test_lora([40, 3, 0, 17], 320, 448, 24, 3, True, True, bound)
