@@ -715,13 +715,15 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs
 //   * Values pass through registers on their way to LDS and are fp16 there, so that p goes to the second product as one fp16 number: as two bf16
 //     numbers beside bf16 values, twice the products, two chunks of 4680 rows took 938 us instead of 694, prompts 456 instead of 298 (one bf16
 //     number: 622 and 271, and 1.4 times the error).  e4m3 and most bf16 are exact in fp16; a tile that holds others is left out by the loop
-//     and taken afterwards as it is, which takes three to four times as long.
+//     and taken afterwards as it is (every 40th page so 797 us instead of 707, all of them 2361).
 //   * Keys of 8 bits are widened on the way too: every wave reads every fragment, and widening those would be eight times the
 //     conversions.  8-bit tiles are fetched one tile earlier.
 template <int NW>
 constexpr int kRowsStages = 65536 + (NW == 8 ? 8 * 8192 : 0);
+// Tiles that are taken apart from the loop and noted by their numbers; if there are more, all from the first to the last are looked at again.
+constexpr int kApartTiles = 48;
 template <int NW>
-constexpr int kRowsLds = kRowsStages<NW> + NW * kApartBytes + 64;      // bytes of LDS
+constexpr int kRowsLds = kRowsStages<NW> + NW * kApartBytes + 64 + 4 * kApartTiles;      // bytes of LDS
 
 template <bool E4M3, int NW>
 __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows_kernel(PagedAttnArgs a) {
@@ -735,8 +737,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
     __shared__ __attribute__((aligned(16))) unsigned char smem[kRowsLds<NW>];
     unsigned char* const k_stage = smem;                      // [2][64 keys][256 B]
     unsigned char* const v_stage = smem + 2 * kTile;          // [2][64 keys][256 B]
-    constexpr int kStages = kRowsStages<NW>;                  // behind them eight waves' rows, then add_apart's scratch and a word per wave
+    constexpr int kStages = kRowsStages<NW>;                  // behind them eight waves' rows, then add_apart's scratch, two words per wave and a list of tiles
     unsigned* const flags = reinterpret_cast<unsigned*>(smem + kStages + NW * kApartBytes);
+    int* const apart = reinterpret_cast<int*>(flags + 16);
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l31 = lane & 31, lh = lane >> 5;
@@ -937,7 +940,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
         for (int db = 0; db < 4; ++db) v_at[db] = R::v_lane(lane, db);
         const float scale = a.mask.scale_log2e;
 
-        int care_first = INT_MAX, care_last = -1;             // tiles whose values are left out by the loop (below)
+        int care_count = 0, care_first = 0, care_last = 0;    // tiles whose values are left out by the loop (below)
         auto nothing = []() {};
         f32x16 s_a[2], s_b[2];
         qk_half(s_a, k_stage, 0, nothing);
@@ -1043,7 +1046,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             l += lsum;
             __builtin_amdgcn_sched_barrier(0);
             if (__builtin_expect(care, 0) && (!E4M3 || masked)) {        // (NaN that every row sees needs none)
-                care_first = min(care_first, n);
+                if (care_count < kApartTiles) apart[care_count] = n;
+                if (care_count++ == 0) care_first = n;
                 care_last = n;
                 return;
             }
@@ -1071,13 +1075,14 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
         // ---- Tiles with values that do not go to the second product like others: bf16 beyond the range of fp16, which are taken as they are
         // here, with p as two bf16 numbers; infinities and NaN in either format, which are added key by key.  Their p is in l already;
         // their scores are formed once more, the same in the same order, and p at the last reference point.  Rare, so short, not fast.
-        for (int n = care_first; n <= care_last; ++n) {
+        const bool listed = care_count <= kApartTiles;
+        for (int i = 0; i < (listed ? care_count : care_last - care_first + 1); ++i) {
             constexpr int C = E4M3 ? kFp16 : kBf16;
-            const int key0 = key_of(n);
             __syncthreads();                     // everyone is done with the stages
+            const int n = listed ? __builtin_amdgcn_readfirstlane(apart[i]) : care_first + i, key0 = key_of(n);
             bool care = false;
-            for (int i = threadIdx.x; i < KT * kRow / 16; i += 64 * NW) {
-                const int r = i / (kRow / 16), c = i % (kRow / 16), key = key0 + r;
+            for (int x = threadIdx.x; x < KT * kRow / 16; x += 64 * NW) {
+                const int r = x / (kRow / 16), c = x % (kRow / 16), key = key0 + r;
                 long long page = table[min(key >> a.batch.page_shift, a.batch.table_stride - 1)];
                 if ((unsigned long long)page >= (unsigned)a.batch.n_pages) page = 0;
                 const long long at = (((page * a.batch.kv_heads + w.hk) << a.batch.page_shift) + (key & slot_mask)) * kRow + c * 16;
@@ -1124,8 +1129,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             }
             __syncthreads();                     // nobody needs those any more
             const unsigned long long all = broken[0] | ((unsigned long long)broken[1] << 32);
-            for (int i = threadIdx.x; i < KT * 16; i += 64 * NW)
-                if ((all >> (i >> 4)) & 1) *reinterpret_cast<uint4*>(v_stage + i * 16) = uint4{0, 0, 0, 0};
+            for (int x = threadIdx.x; x < KT * 16; x += 64 * NW)
+                if ((all >> (x >> 4)) & 1) *reinterpret_cast<uint4*>(v_stage + x * 16) = uint4{0, 0, 0, 0};
             __syncthreads();
 #pragma unroll
             for (int ts = 0; ts < 4; ++ts) {

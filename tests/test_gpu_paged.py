@@ -476,6 +476,18 @@ def test_values_at_the_ends_of_fp16(form, size):
     close(o, want, BF16 * want.abs() + 2.0 ** -10 * mass)
 
 
+@pytest.mark.parametrize("every", [1, 9])
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_values_beyond_fp16_in_many_tiles(form, every):
+    c = Cache([140, 1], [5000, 4100], 1, 16, seed=2, spare=0).fill(4)
+    c.v[::every] *= 2.0 ** 10                    # fp16 holds those times 2^8 up to 2^16
+    q = randn(6, c.T, 4 * D)
+    for block, window, sink in ((1, 0, 0), (0, 4000, 64)):
+        o = run_attention(c, q, 4, block, window, sink)
+        want, mass = attention_64(c, q, 4, block, window, sink)
+        close(o, want, BF16 * want.abs() + 2.0 ** -10 * mass)
+
+
 @pytest.mark.parametrize("form", FORMS, indirect=True)
 def test_infinite_values_that_every_row_sees(form):
     """They come out as the formula has them: an infinity stays one, two of opposite sign and NaN are NaN; the other channels and the
