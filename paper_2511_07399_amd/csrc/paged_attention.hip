@@ -292,30 +292,30 @@ __device__ __forceinline__ unsigned broken_keys(const unsigned char* v, int firs
 
 // Adds to O^T the keys in `broken` of 32 (rows `first` .. of the value tile), one by one and only to the rows that see them: in a product
 // with the others, zero times their infinities or NaN would reach rows that do not, and an infinity times p's second piece would be
-// NaN where p times it is not.  w0, w1: p of the 32 keys; sees(j): whether this lane's row sees key j.  scratch: 2 KB of the wave's.
-// The caller then blanks these keys' values and goes on as ever.  Rare, so short, not fast.
+// NaN where p times it is not.  w0, w1: p of the 32 keys, s: their scores, minus infinity where the row does not see the key.  scratch: 2 KB of
+// the wave's.  The caller then blanks these keys' values and goes on as ever.  Rare, so short, not fast.
 constexpr int kApartBytes = 2048;
-template <int F, typename S>
-__device__ __forceinline__ void add_apart(f32x16 (&o)[4], const unsigned char* v, int first, const Weights<F>& w0, const Weights<F>& w1, unsigned broken,
-                                          unsigned char* scratch, int lane, S&& sees) {
+template <int F>
+__device__ __forceinline__ void add_apart(f32x16 (&o)[4], const unsigned char* v, int first, const Weights<F>& w0, const Weights<F>& w1, const f32x16& s,
+                                          unsigned broken, unsigned char* scratch, int lane) {
     typedef Rows<F> R;
     const int lh = lane >> 5;
-    float* const own = reinterpret_cast<float*>(scratch);     // [eight keys of sixteen][64 lanes]
+    float* const own = reinterpret_cast<float*>(scratch);     // [eight keys of sixteen][64 lanes]; -1: not seen
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
         unsigned left = broken >> (16 * half) & 0xffffu;
         if (left == 0) continue;
         reads_done();                                         // (of what lay there)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) own[e * 64 + lane] = half == 0 ? w0.get(e) : w1.get(e);
+        for (int e = 0; e < 8; ++e) own[e * 64 + lane] = s[8 * half + e] == -INFINITY ? -1.0f : half == 0 ? w0.get(e) : w1.get(e);
         hold_order();
 #pragma clang loop unroll(disable)
         while (left != 0) {
             const int j = __builtin_ctz(left), row = first + 16 * half + j;
             left &= left - 1;
-            const unsigned keep = sees(16 * half + j) ? ~0u : 0u;
             // key j of sixteen: element (j & 3) + 4 (j / 8) of lane half j / 4 % 2
             const float p = own[((j & 3) + 4 * (j >> 3)) * 64 + (lane & 31) + 32 * ((j >> 2) & 1)];
+            const unsigned keep = p >= 0.0f ? ~0u : 0u;
 #pragma unroll
             for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -545,8 +545,7 @@ again:
             hold_order();
             const unsigned broken = masked || careful ? broken_keys<F>(vt, 0, lane) : 0u;
             if (__builtin_expect(broken != 0, 0)) {
-                add_apart<F>(o, vt, 0, pf[0], pf[1], broken, smem + kTokenStages + wave * kApartBytes, lane,
-                             [&](int j) { return sees(keys, key0 + j) & (((gaps >> (j >> 4)) & 1) == 0); });
+                add_apart<F>(o, vt, 0, pf[0], pf[1], s0, broken, smem + kTokenStages + wave * kApartBytes, lane);
                 if ((broken >> l31) & 1)
                     for (int c = 0; c < R::kRow / 32; ++c) *reinterpret_cast<uint4*>(vt + l31 * R::kRow + lh * (R::kRow / 2) + c * 16) = uint4{0, 0, 0, 0};
                 reads_done();
@@ -1112,20 +1111,19 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
             qk_half(s_a, k_stage, 0, nothing);
             qk_half(s_a, k_stage, 1, nothing);
             const RowKeys keys = row_keys(a.mask, place_of(own_row()).token, w.n, w.kv_len);
-            auto seen = [&](int j) { return sees(keys, key0 + j) & (((gaps >> (j >> 4)) & 1) == 0); };
             Weights<C> p[4];
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int j = 8 * (i >> 2) + (i & 3) + 4 * lh;
-                const float x = seen(j) ? s_a[i >> 4][i & 15] : -INFINITY;
-                p[i >> 3].set(i & 7, __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -m)) * (E4M3 ? 1.0f : kValueScale));
+            for (int r = 0; r < 32; ++r) {
+                const int j = 8 * (r >> 2) + (r & 3) + 4 * lh;
+                const bool seen = sees(keys, key0 + j) & (((gaps >> (j >> 4)) & 1) == 0);
+                const float x = s_a[r >> 4][r & 15] = seen ? s_a[r >> 4][r & 15] : -INFINITY;
+                p[r >> 3].set(r & 7, __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale, -m)) * (E4M3 ? 1.0f : kValueScale));
             }
             unsigned broken[2];
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
                 broken[kb] = broken_keys<C>(v_stage, 32 * kb, lane);
-                add_apart<C>(o, v_stage, 32 * kb, p[2 * kb], p[2 * kb + 1], broken[kb], smem + kStages + wave * kApartBytes, lane,
-                             [&](int j) { return seen(32 * kb + j); });
+                add_apart<C>(o, v_stage, 32 * kb, p[2 * kb], p[2 * kb + 1], s_a[kb], broken[kb], smem + kStages + wave * kApartBytes, lane);
             }
             __syncthreads();                     // nobody needs those any more
             const unsigned long long all = broken[0] | ((unsigned long long)broken[1] << 32);

@@ -507,6 +507,31 @@ def test_infinite_values_that_every_row_sees(form):
     close(o[rest], clean.view(c.T, 8, D)[rest], tol.view(c.T, 8, D)[rest], "what is not broken")
 
 
+@pytest.mark.parametrize("form", FORMS, indirect=True)
+def test_scores_of_minus_infinity_weigh_nothing(form):
+    """Whatever the values of such keys are; a row that has no other score is the zero row."""
+    c = Cache([100, 3], [300, 40], 1, 16, seed=4).fill(2)
+    q = randn(3, c.T, 2 * D)
+    q[:, :D] = q[:, :D].abs()                    # head 0: minus infinity everywhere in sequence 1; head 1 there: plus, which is NaN
+    q[:, D:] = -q[:, D:].abs()
+    q[:100] = randn(4, 100, 2 * D)
+    q[:100, 5], q[:100, D + 5] = 1.0, 1.0        # sequence 0: minus infinity of six keys
+    inf = float("inf")
+    hit = (0, 17, 64, 65, 130, 222)
+    for j in hit:
+        c.k[c.table[0, j // 16], 0, j % 16, 5] = -inf
+        c.v[c.table[0, j // 16], 0, j % 16] = inf if j % 2 else float("nan")
+    for j in range(40):
+        c.k[c.table[1, j // 16], 0, j % 16, 7] = -inf
+        c.v[c.table[1, j // 16], 0, j % 16, 9] = inf
+    o = run_attention(c, q, 2, 0, 0, 0)
+    for j in hit:                                # as if they were not there
+        c.k[c.table[0, j // 16], 0, j % 16, 5], c.v[c.table[0, j // 16], 0, j % 16] = -3e4, 0.0
+    want, mass = attention_64(c, q, 2, 0, 0, 0)
+    close(o[:100], want[:100], (BF16 * want.abs() + 2.0 ** -10 * mass)[:100])
+    assert (o[100:, :D] == 0).all() and o[100:, D:].isnan().all()
+
+
 def test_attention_offsets_beyond_32_bits():
     # a pool of 4.5 GiB, of which the last pages are used
     page, heads = 256, 8
