@@ -105,10 +105,20 @@ __global__ __launch_bounds__(256) void turn_kernel(TurnArgs a, int waves_per_row
         if (kind < 2) {
             const float* gain = kind == 0 ? a.g_q : a.g_k;
             if (gain != nullptr) {
-                float sq = 0.0f;
+                auto squares = [&]() {
+                    float sq = 0.0f;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sq += x[e] * x[e];
-                const float r = rsqrtf(head_sum(sq) * (1.0f / kHeadDim) + a.eps);
+                    for (int e = 0; e < 8; ++e) sq += x[e] * x[e];
+                    return head_sum(sq) * (1.0f / kHeadDim);
+                };
+                float mean = squares(), eps = a.eps;
+                if (__builtin_expect(mean == INFINITY, 0)) {                  // beyond 32 bits: the head times 2^-70, and eps with it
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] *= 0x1p-70f;
+                    mean = squares();
+                    eps *= 0x1p-140f;
+                }
+                const float r = rsqrtf(mean + eps);
                 const f32x4 g0 = *reinterpret_cast<const f32x4*>(gain + c * 8), g1 = *reinterpret_cast<const f32x4*>(gain + c * 8 + 4);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) x[e] *= r * (e < 4 ? g0[e & 3] : g1[e & 3]);

@@ -115,6 +115,23 @@ def test_norm_rope_of_zero_huge_and_broken_heads():
     close(out.view(4, 4, D).cpu()[keep], want.view(4, 4, D)[keep], (BF16 * want.abs() + TURN * size).view(4, 4, D)[keep])
 
 
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("size", [1e17, 1e18, 1e20, 1e30, 3e38])
+def test_norm_of_heads_whose_squares_are_beyond_32_bits(size, halves):
+    x = randn(4, 9, 5 * D).float().clamp(-1, 1)
+    x[:, :D], x[4, 3 * D:] = x[:, :D] * size, x[4, 3 * D:] * size
+    x = x.to(torch.bfloat16)
+    x[6, D + 7] = float("inf")                  # its own place NaN, the head's others zero
+    pos, g, out = ints([[3 * i] for i in range(9)]), 1.0 + randn(5, D, dtype=torch.float32, scale=0.2), torch.empty_like(x)
+    b.qk_norm_rope(b.rope_cfg(1, halves=halves), pos, x, out, g)
+    want, length = turned(x, g, pos, 1, halves)
+    sound = torch.ones(9, 5, dtype=torch.bool)
+    sound[6, 1] = False
+    close(out.view(9, 5, D).cpu()[sound], want.view(9, 5, D)[sound], (BF16 * want.abs() + TURN * length).view(9, 5, D)[sound])
+    broken = out.view(9, 5, D)[6, 1].float().cpu()
+    assert torch.equal(broken.isnan(), want.view(9, 5, D)[6, 1].isnan()) and (broken[~broken.isnan()] == 0).all()
+
+
 # ------------------------------------------------------------------------------------------ pages
 class Cache:
     """A pool whose pages are handed out in random order; slots nobody has written hold NaN (`poison`)."""
