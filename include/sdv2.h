@@ -637,7 +637,8 @@ int32_t sdv2_paged_append(const sdv2_paged_cfg* cfg, void* k_pages_dev, void* v_
  *   see them (infinities, NaN, storage never written) does not reach it.
  *   scale <= 0: 1 / sqrt(128).  scale log2(e) k_scale: not 0 or infinite in 32 bits.  Scores (scale q k) of up to 2^29 in size, values of up to 2^90.  o overlaps none of what is read.
  *   Scores, weights and sums are held in 32 bits; a weight goes to the product with the values as a number of at least 11 bits.
- * sdv2_paged_attention_workspace_bytes: for few rows and many keys, which are then shared out over the chip (0 where they are not).
+ * sdv2_paged_attention_workspace_bytes: for few rows and many keys, which are then shared out over the chip (0 where they are not).  Of the
+ *   batch as given: a smaller one may need more.
  * ------------------------------------------------------------------------------------------------ */
 typedef struct sdv2_attn_mask {
     uint32_t struct_size;

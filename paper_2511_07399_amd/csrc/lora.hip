@@ -3,7 +3,8 @@
 //
 // Memory bound: x, y, out and the adapters' matrices once, 2 r (K + N) flops a row.  Two launches with u = scale x A^T between them, on
 // 16x16x32 matrix instructions.  (One launch, in which each workgroup of the second product forms u for itself, reads A once per
-// workgroup: 64 tokens of rank 16, 5120 to 15 360, 12.3 us instead of 13.2, but 8 of rank 64, 5120 x 5120, 36 instead of 12.)
+// workgroup: when both were built, 64 tokens of rank 16, 5120 to 15 360, took 12.3 us instead of 13.2, but 8 of rank 64, 5120 x 5120, 36 instead
+// of 12.)  Times below: a pass among others in a recorded graph.
 //   u: computed transposed, ranks as rows and tokens as columns.  Few tokens: lora_down_kernel, 16 tokens and 16 ranks a workgroup, its
 //     eight waves in turn over pieces of 64 of K, K in parts over workgroups.  Many: lora_down_tile_kernel, 32 tokens.  u stays in 32
 //     bits, and goes to the second product as two or three bf16 numbers that add up to it (kPieces: as one, its rounding would be the
@@ -11,7 +12,7 @@
 //   out: lora_up_kernel, tokens as rows, y as the accumulator's start; one or two tokens a sequence: lora_up_few_kernel, on the vector unit.
 // What the cache is asked for a load decides: 16 bytes of a lane are an access by themselves unless the lanes next to it are in the same
 // line.  8800 tokens of four sequences, bf16, 5120 x 5120 of rank 64: fragments straight from memory 145 us, rows by lines through LDS 97
-// (270 MB in 46 + 53 us, 2.7 TB/s); 1536 x 1536 45 -> 32; 32 bits, 5120 x 5120, 175 -> 119 (3.8 TB/s).
+// (now 100: 270 MB, 2.7 TB/s); 1536 x 1536 45 -> 32 (now 33.5); 32 bits, 5120 x 5120, 175 -> 119 (now 121: 3.7 TB/s).
 #include "ragged.h"
 
 #include <type_traits>
@@ -358,8 +359,9 @@ __global__ __launch_bounds__(256, lora_up_waves(KS, sizeof(T))) void lora_up_ker
 // One or two tokens of a sequence: on the vector unit, where a tile would be empty but for those of sixteen tokens.  B's rows lie one behind the
 // other, so lanes next to each other read pieces of eight ranks next to each other: P lanes have a column (P the power of two from the
 // pieces of a row on), 64 / P columns a load, and add up by moves within the row of lanes; of the P loads that cover 64 columns a lane
-// keeps the sum of one, its own.  B's bytes bound it: 64 tokens of 16 adapters beside 5120 x 15 360, both launches, rank 16 15.2 us, 64
-// 31.2, 128 48.4 (by tiles 18.5, -, 59.5; a lane with columns of its own, 16 bytes of 64 lines a load, 15.0 and 48.6 at ranks 16 and 64).
+// keeps the sum of one, its own.  B's bytes bound it: 64 tokens of 16 adapters beside 5120 x 15 360, both launches, rank 16 15.1 us, 64
+// 30.9, 128 52.6 (by tiles 20.7, 39.9 and 66.4; a lane with columns of its own, 16 bytes of 64 lines a load, when this was 15.3 and 31.2 us, 15.0 and
+// 48.6 at ranks 16 and 64).
 template <int P>
 __device__ __forceinline__ float piece_sum(float v) {
     if (P >= 2) v += dpp_f<0xB1>(v);         // quad_perm [1, 0, 3, 2]
@@ -435,9 +437,9 @@ __global__ __launch_bounds__(256) void lora_up_few_kernel(LoraArgs a, unsigned g
 }
 
 // Tiles of sixteen tokens and ranks, K in parts, for one or two tokens a sequence and wherever that is under half a workgroup a compute unit; else
-// tiles of 32 tokens by lines.  Measured, by sixteens | by 32 in us, 5120 x 5120: 16 sequences of 4 tokens of rank 16 10.0 | 13.5, of 48
-// 13.9 | 19.5; one of 1000 of rank 128 38.7 | 32.6; 128 of 16 of rank 16 30.2 | 25.6; 1536 x 4608: 100 of 4 14.7 | 15.5, of 16 17.5 | 17.4,
-// 64 of 24 of rank 64 26.0 | 23.1, 64 of 16 19.6 | 20.1.
+// tiles of 32 tokens by lines.  Measured, by sixteens | by 32 in us, 5120 x 5120: 16 sequences of 4 tokens of rank 16 10.3 | 14.9, of 48
+// 13.9 | 19.7; one of 1000 of rank 128 40.3 | 34.4; 128 of 16 of rank 16 30.3 | 26.2; 1536 x 4608: 100 of 4 15.1 | 16.2, of 16 17.9 | 17.8,
+// 64 of 24 of rank 64 28.4 | 25.4, 64 of 16 20.6 | 21.5.
 int sixteens(int n_seqs, int n_tokens, int rank) { return max(n_tokens / 16, n_seqs) * ((rank + 15) / 16); }
 bool by_sixteens(int n_seqs, int n_tokens, int max_q_len, int rank) { return lora_by_tokens(max_q_len) || sixteens(n_seqs, n_tokens, rank) < kUnits / 2; }
 

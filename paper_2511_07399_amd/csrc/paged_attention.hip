@@ -7,7 +7,7 @@
 // matrix cores.  Two kernels, each in one pass with the running reference point and sum of a softmax, and a third that
 // joins parts of a key range.  Measured (32 query and 8 key heads unless said otherwise):
 //   few rows: 64 tokens over 1 to 16 000 keys 1.99 GB in 365 us, 5.45 TB/s (reads of 8 KB at random places alone: 6.05); 8-bit pages,
-//     0.99 GB, 194 us, 5.1 TB/s; one token over 9001 keys 14.5 us in two launches.
+//     0.99 GB, 194 us, 5.1 TB/s; one token over 9001 keys 14.9 us in two launches.
 //   many rows: 2 x 4680 rows of 12 heads over 10 920 keys 628 GF in 694 us, 0.9 PF/s (the kernel over contiguous keys, whose values lie
 //     transposed already and whose p is one bf16 number, 1.2); six prompts of 1 to 4096 tokens, causal, 234 GF in 298 us: the last
 //     workgroups' tail; 333 rows over 32 700 keys of 8 bits 179 GF in 207 us, the join's reading included.
@@ -708,7 +708,8 @@ __global__ __launch_bounds__(256) void paged_attention_join_kernel(PagedAttnArgs
 //   * Scores are computed transposed, S^T = K Q^T: a lane owns a row (column of S^T) with its partner lane + 32, keeps the row's sum and
 //     reference point, and the accumulators are in the order that the second product O^T = V^T P^T takes its P in.
 //   * Keys and values have two stages each.  While the vector unit forms p of tile n, the matrix unit forms S^T of tile n + 1; then
-//     come the values of tile n.  The loads of keys n + 2 and values n + 1 go out between the first products.
+//     come the values of tile n.  The loads of keys and values n + 2 go out between the first products, those to LDS and these to
+//     registers, from which they are put into LDS at the start of the next tile.
 //   * The reference point of a row's exponents trails its maximum by up to kSumLimit's logarithm: a steady tile forms no maximum and
 //     rescales nothing.
 //   * Values pass through registers on their way to LDS and are fp16 there, so that p goes to the second product as one fp16 number: as two bf16
@@ -1159,9 +1160,10 @@ void set_paged_overrides(int rows, int parts) {
 // after the units with one; many small parts even that out and even out the lengths, which only the device knows.  A part costs a
 // workgroup's start (4 us) and the join's reading: it is worth 512 keys (8-bit pages, half the bytes: 1024).  With less than a
 // workgroup per unit the chain of a workgroup's tiles is the time, and 128 keys, one tile a wave, are worth a part.  us, bf16, 8 key
-// heads, equal lengths, this rule / best number of parts: 64 x 7584 keys 351 / 335, 32 x 12 000 282 / 270, 32 x 700 24.9 / 23.3, 12 x 3000
-// 38.7 / 35.0, 4 x 3000 17.3 / 17.3, 4 x 700 11.7 / 11.7, 1 x 12 000 17.5 / 17.4, 1 x 3000 12.4 / 12.4.  64 x 1 to 16 000: 363 / 363, one
-// part 387; of 8 bits 194 / 194, one part 214.
+// heads, equal lengths, this rule / best number of parts: 64 x 7584 keys 362 / 337 (one), 32 x 12 000 293 / 271 (three; one 349), 32 x 700 26.1 / 23.7
+// (two), 12 x 3000 36.4 / 35.7, 4 x 3000 17.5 / 17.4 (eight; one 35.5), 4 x 700 12.7 / 11.9, 1 x 12 000 17.6 / 17.6 (32; one 117), 1 x 3000 13.4 / 12.7.
+// 64 x 1 to 16 000: 385 / 366 (eight), one part 392; of 8 bits 205 / 199 (six), one 214.  Equal lengths want few parts and ragged ones more,
+// and the host knows the longest only.
 static int token_parts(long long workgroups, int keys, int e4m3) {
     const long long spread = min((4096 + workgroups - 1) / workgroups, (long long)(keys / (e4m3 ? 1024 : 512)));
     const long long chain = min(kUnits / workgroups, (long long)(keys / 128));
@@ -1172,9 +1174,12 @@ static int token_parts(long long workgroups, int keys, int e4m3) {
 //   rounds (tiles per + start), rounds of `slots` workgroups, the last by how much of it is filled (two workgroups on a unit share it),
 //   or the keys' bytes at `rate` where that is longer,  + join per part and its bytes.
 // Fitted to 1056 launches of 38 shapes (100 to 9360 rows times 1 to 8 in a group, 700 to 33 000 keys, 1 to 40 key heads, both formats, every
-// form in 1 to 32 parts): rms error 15 %, and the form picked is on average 2 % slower than the best of all.  What it replaced, 128 rows up
-// to 128 and 256 beyond in as many parts as fill the units: 8 x 64 new tokens over 8000 keys 135.6 -> 103.3, 3 x 200 over 12 000
-// 236.9 -> 146.4, of 8 bits 8 x 16 over 8000 79.0 -> 47.7, 333 over 33 000 333 -> 209.
+// form in 1 to 32 parts) when p was one bf16 number: rms error 15 %, the form picked 2 % slower than the best of all in the mean.  Of the
+// present kernels (bf16 pages 10 to 20 % slower in every form) over 98 shapes of both formats drawn afterwards, 12 to 2500 rows a sequence: 6.6 % slower
+// in the mean; a new fit to those was no better on shapes of yet another draw.  The largest losses, up to 60 %, are where the estimate
+// has the workgroups just fill the units: numbers that no row tile has take places too.  What it replaced, 128 rows up to 128 and
+// 256 beyond in as many parts as fill the units (both then): 8 x 64 new tokens over 8000 keys 135.6 -> 103.3, 3 x 200 over 12 000 236.9 -> 146.4,
+// of 8 bits 8 x 16 over 8000 79.0 -> 47.7, 333 over 33 000 333 -> 209.
 struct FormCost {
     int rows, keys, slots;
     float two, one, start, rate;      // a tile of keys (of the four waves, where they share them out) with both slots of a unit taken and with one

@@ -129,6 +129,16 @@ def test_mask_refusals(lib, bad):
     assert attend(lib, cfg(), batch(), None) == INVALID
 
 
+@pytest.mark.parametrize("e4m3", [0, 1])
+def test_attention_that_is_shared_out_needs_its_workspace(lib, e4m3):
+    c, long = cfg(format=e4m3), batch(n_seqs=1, n_tokens=1, max_q_len=1, max_kv_len=60000, table_stride=4000)
+    need = lib.sdv2_paged_attention_workspace_bytes(ref(c), ref(long), ref(mask()), 4)
+    assert need >= 2 * 4 * 130 * 4                  # two parts at least, of four rows of heads
+    assert attend(lib, c, long, mask(), ws=P, ws_bytes=need - 1) == SMALL
+    assert attend(lib, c, long, mask(), ws=None, ws_bytes=need) == SMALL
+    assert attend(lib, c, long, mask(), ws=P + 8, ws_bytes=need) == INVALID
+
+
 @pytest.mark.parametrize("scale,k_scale", [(1e-20, 1e-30), (1e-30, 1e-20), (1e20, 1e30), (3e38, 1.0)])
 def test_a_scale_of_zero_or_infinity_with_the_keys_scale_is_refused(lib, scale, k_scale):
     """Times the keys' scale it multiplies masked scores, minus infinity: zero would make them NaN."""
