@@ -948,7 +948,8 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 2 : 1) void paged_attention_rows
 
         // One tile: s_cur holds S^T of tile n; S^T of tile n + 1 is formed into s_nxt on the way.  k_now: keys n + 1; k_fill: keys n + 2 go there;
         // v_now: values n; v_fill: values n + 1 go there (restrict: a transposing read is taken to wait for every load on its way to LDS
-        // that may alias it); care_now, care_fill: the words of the values n and n + 1.  Past the last tile it is fetched again, unconditionally, into a stage that nobody reads.
+        // that may alias it); care_now, care_fill: the words of the values n and n + 1.  Past the last tile it is fetched again,
+        // unconditionally, into a stage that nobody reads.
         auto tile_step = [&](const unsigned char* __restrict__ k_now, unsigned char* __restrict__ k_fill, unsigned char* __restrict__ v_now,
                              unsigned char* __restrict__ v_fill, f32x16 (&s_cur)[2], f32x16 (&s_nxt)[2], int n, const unsigned* __restrict__ care_now,
                              unsigned* __restrict__ care_fill) __attribute__((always_inline)) {
